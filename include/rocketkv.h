@@ -84,7 +84,10 @@ typedef enum {
   ROCKETKV_OP_HSA_DECODE = 0,   /* a = token_budget                       */
   ROCKETKV_OP_DENSE_DECODE = 1, /* no extra arguments                     */
   ROCKETKV_OP_SNAPKV = 2,       /* a = window, b = keep_budget            */
-  ROCKETKV_OP_ATTEND = 3        /* a = pages_row_len (0 = every page)     */
+  ROCKETKV_OP_ATTEND = 3,       /* a = pages_row_len (0 = every page)     */
+  ROCKETKV_OP_APPEND_CHUNK = 4, /* a = n_tokens                           */
+  ROCKETKV_OP_CHUNK_ATTEND = 5, /* a = n_tokens                           */
+  ROCKETKV_OP_WEIGHT_EVICT = 6  /* a = n_recent, b = keep_budget          */
 } rocketkv_op_t;
 
 typedef enum {
@@ -336,6 +339,127 @@ int32_t rocketkv_mt_hsa_decode_append(const rocketkv_cache_t* cache, const rocke
                                       int32_t n_recent_pages, void* out, float* out_lse,
                                       int32_t* out_pages, int32_t* out_channels, void* workspace,
                                       size_t workspace_bytes, void* stream);
+
+/*
+ * A chunk: the new tokens of all sequences of a cache, packed one behind the other.  Row r of a packed
+ * tensor is one token; rows starts[b] .. starts[b+1]-1 belong to sequence b, in order.  A sequence may bring
+ * no row, one, or a whole prompt.  starts is ascending from >= 0 to <= n_tokens; rows in front of starts[0] and behind
+ * starts[batch] are neither read nor written.  The struct lives in host memory, starts on the device.  (Entries that
+ * descend or leave [0, n_tokens] cut a sequence's rows short; no call leaves its buffers for them.)
+ */
+#define ROCKETKV_MAX_CHUNK (1 << 24)
+typedef struct rocketkv_chunk {
+  int32_t n_tokens;      /* rows of the packed tensors, at most ROCKETKV_MAX_CHUNK */
+  const int32_t* starts; /* device [batch + 1] */
+} rocketkv_chunk_t;
+
+/*
+ * Rotary positions: of the leading rot_dim channels of a head, pair i is turned by the angle
+ * position * inv_freq[i]:
+ *   (x, y) -> scale * (x cos - y sin, y cos + x sin)
+ * where pair i is channels (i, i + rot_dim / 2), or (2i, 2i + 1) with `interleaved`; the other channels pass through.
+ * Angles are formed and reduced in 64 bits, the rotation is computed in fp32 and rounded to bf16 once.
+ */
+typedef struct rocketkv_rope {
+  int32_t rot_dim;        /* even, 2 .. head_dim */
+  int32_t interleaved;    /* 0 or 1 */
+  const double* inv_freq; /* device [rot_dim / 2]: radians per position */
+  float scale;            /* factor of the turned channels, 1 without scaling */
+} rocketkv_rope_t;
+
+/*
+ * Frequencies for rotary positions, stretched for contexts longer than a model was trained on (host arithmetic in double
+ * precision).  With f[i] = theta^(-2i / rot_dim):
+ *   PLAIN   f[i]
+ *   LINEAR  f[i] / factor                             positions interpolated
+ *   BASE    theta replaced by theta * factor^(rot_dim / (rot_dim - 2)): the lowest frequency divided by factor, the
+ *           highest unchanged (rot_dim > 2)
+ *   BANDS   by turns t = original * f[i] / 2 pi over the original context: f[i] where t >= high, f[i] / factor where
+ *           t <= low, and between them (1 - u) f[i] / factor + u f[i], u = (t - low) / (high - low)
+ *   RAMP    the same mixture by the pair's index: u = 1 - clamp((i - a) / (b - a), 0, 1) where a, b are the indices at
+ *           which a frequency makes `high` and `low` turns, rounded down and up, in [0, rot_dim - 1] (b at least
+ *           a + 0.001); *scale = 0.1 ln(factor) + 1
+ * *scale is 1 but for RAMP.  factor >= 1; BANDS and RAMP need 0 < low < high and original >= 1.
+ */
+typedef enum {
+  ROCKETKV_ROPE_PLAIN = 0,
+  ROCKETKV_ROPE_LINEAR = 1,
+  ROCKETKV_ROPE_BASE = 2,
+  ROCKETKV_ROPE_BANDS = 3,
+  ROCKETKV_ROPE_RAMP = 4
+} rocketkv_rope_kind_t;
+int32_t rocketkv_rope_frequencies(int32_t kind, int32_t rot_dim, double theta, double factor, double low, double high,
+                                  int64_t original, double* inv_freq /* host [rot_dim / 2] */, float* scale /* host */);
+
+/*
+ * Rotary positions of packed head rows: head h of token t is at x + t * x_stride + h * head_dim and goes to
+ * y + t * y_stride + h * head_dim (bf16, head_dim 128; strides in elements, multiples of 8 and at least
+ * n_heads * head_dim; x and y 16-byte aligned).  x == y with equal strides turns in place; other overlaps are not
+ * allowed.  positions: device int32 [n_tokens], any value.
+ */
+int32_t rocketkv_rope(const rocketkv_rope_t* rope, const int32_t* positions, int32_t n_tokens, int32_t n_heads,
+                      const void* x, int64_t x_stride, void* y, int64_t y_stride, void* stream);
+
+/*
+ * A chunk's tokens into the cache: token i of sequence b goes to position seq_lens[b] + i, its key turned by `rope`
+ * (NULL: as it is), and seq_lens[b] grows by the sequence's rows.  The caches, summaries and lengths end up as after
+ * rocketkv_append_kv of the (turned) tokens one by one, but that a sequence without room for all of its rows is left
+ * unchanged.  Where q is given, the queries of all rows are turned into q_out as well.
+ * q: bf16, token r at q + r * q_stride (n_q_heads heads); q_out: bf16 [n_tokens][n_q_heads][head_dim], may be q itself if
+ *    q_stride is n_q_heads * head_dim; both NULL: no queries.
+ * k_new, v_new: bf16, token r at + r * k_stride / v_stride (n_kv_heads heads).  Strides as in rocketkv_rope, so that all
+ *    three may lie in the rows of one joint projection.
+ * positions: device int32 [n_tokens] or NULL: a token's position in the cache (after an eviction the two differ).
+ * kmax, kmin: both, or both NULL where no summaries are kept (RocketKV-MT builds them from the next filter).
+ * Channel-major V needs page_size 16.
+ * workspace: rocketkv_workspace_bytes(ROCKETKV_OP_APPEND_CHUNK, cache, n_tokens, 0).
+ */
+int32_t rocketkv_append_chunk(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const rocketkv_rope_t* rope,
+                              const int32_t* positions, const void* q, int64_t q_stride, void* q_out, const void* k_new,
+                              int64_t k_stride, const void* v_new, int64_t v_stride, void* kmax, void* kmin,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Causal attention of a chunk whose tokens are in the cache already: row i of the n rows of sequence b attends to the
+ * tokens at positions 0 .. seq_lens[b] - n + i (scale 1/sqrt(head_dim)); bf16 operands, fp32 logits, softmax and sums,
+ * bf16 result.  Whole prompts (seq_lens[b] == n), pieces of prompts, turns and single tokens mix freely.
+ * q, out: bf16 [n_tokens][n_q_heads][head_dim].  out_lse: optional fp32 [n_tokens][n_q_heads], natural-log sum-exp of the
+ * scaled logits.  Absent pages are skipped; a row with nothing to attend to gets zeros and -inf.
+ * A cached value of a row's future that is not finite reaches the rows of its own chunk that share its 64 tokens.
+ * workspace: rocketkv_workspace_bytes(ROCKETKV_OP_CHUNK_ATTEND, cache, n_tokens, 0).
+ */
+int32_t rocketkv_chunk_attend(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const void* q, void* out,
+                              float* out_lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The attention weight every cached token has received so far:
+ *   weights_out[b][g][j] = (j < seq_lens[b] - n ? weights_in[b][g][j] : 0)
+ *                        + sum over the group's heads h and the chunk's rows i that see j of
+ *                          exp(q[i][h] . K[j] / sqrt(head_dim) - lse[i][h])
+ * for j < seq_lens[b]; later entries are left as they were.  weights: fp32 [batch][n_kv_heads][pages_cap * page_size].
+ * weights_in NULL counts as zeros and may be weights_out itself.  q and lse: as given to and left by
+ * rocketkv_chunk_attend (or, with a chunk of one token per sequence, by rocketkv_dense_decode); a row whose lse is -inf
+ * adds nothing, nor does a token in an absent page receive any.
+ */
+int32_t rocketkv_accumulate_weights(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const void* q,
+                                    const float* lse, const float* weights_in, float* weights_out, void* stream);
+
+/*
+ * Eviction by accumulated weight.  Per (sequence, KV head) of S = src->seq_lens[b] tokens: all are kept if
+ * S <= keep_budget; otherwise the last n_recent tokens and, of the others, the keep_budget - n_recent with the largest
+ * weight (ties: lower position; NaN counts as larger than every number).  K, V and weights of the kept tokens go to
+ * `dst`, in ascending position, and dst->seq_lens[b] = min(S, keep_budget).  src is left as it is.
+ * weights: fp32 [batch][n_kv_heads][src->pages_cap * src->page_size].
+ * dst: a cache with pools and lengths of its own, the same head counts, room for keep_budget tokens, any page size and
+ *      V layout (channel-major: page_size 16, for src as well).
+ * dst_weights: optional fp32 [batch][n_kv_heads][dst->pages_cap * dst->page_size], distinct from weights; the first
+ *      min(S, keep_budget) entries of a row are written.
+ * kept_idx: optional int32 [batch][n_kv_heads][keep_budget], -1 padded.
+ * workspace: rocketkv_workspace_bytes(ROCKETKV_OP_WEIGHT_EVICT, src, n_recent, keep_budget).
+ */
+int32_t rocketkv_weight_evict(const rocketkv_cache_t* src, const float* weights, int32_t n_recent, int32_t keep_budget,
+                              const rocketkv_cache_t* dst, float* dst_weights, int32_t* kept_idx, void* workspace,
+                              size_t workspace_bytes, void* stream);
 
 /*
  * Adaptive compression decomposition (Section 3.6): for a sequence of seq_len

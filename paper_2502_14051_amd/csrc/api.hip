@@ -209,6 +209,14 @@ size_t rocketkv_workspace_bytes(int32_t op, const rocketkv_cache_t* cache, int32
     case ROCKETKV_OP_SNAPKV:
       if (a < 1 || b <= a) { fail(ROCKETKV_INVALID_ARG, "rocketkv_workspace_bytes: need 1 <= window < keep_budget"); return 0; }
       return plan_snapkv(v, a, b).total_bytes;
+    case ROCKETKV_OP_APPEND_CHUNK:
+    case ROCKETKV_OP_CHUNK_ATTEND:
+      if (a < 0) { fail(ROCKETKV_INVALID_ARG, "rocketkv_workspace_bytes: n_tokens must be >= 0"); return 0; }
+      if (a > ROCKETKV_MAX_CHUNK) { fail(ROCKETKV_UNSUPPORTED, "rocketkv_workspace_bytes: n_tokens %d exceeds %d", a, ROCKETKV_MAX_CHUNK); return 0; }
+      return op == ROCKETKV_OP_APPEND_CHUNK ? (size_t)ROCKETKV_WS_HEADER_BYTES : plan_chunk_attend(v, a).total_bytes;
+    case ROCKETKV_OP_WEIGHT_EVICT:
+      if (a < 0 || b < 1 || a > b) { fail(ROCKETKV_INVALID_ARG, "rocketkv_workspace_bytes: need 0 <= n_recent <= keep_budget, keep_budget >= 1"); return 0; }
+      return plan_evict(v, b).total_bytes;
     default:
       fail(ROCKETKV_INVALID_ARG, "rocketkv_workspace_bytes: unknown op %d", op);
       return 0;
@@ -762,6 +770,208 @@ int32_t rocketkv_mt_hsa_decode_append(const rocketkv_cache_t* cache, const rocke
   return mt_decode_impl(who, cache, index, q, k_new, v_new, kmax, kmin, channel_budget, token_budget,
                         n_recent_pages, out, out_lse, out_pages, out_channels, workspace, workspace_bytes,
                         stream);
+}
+
+}  // extern "C"
+
+// ---- a chunk of new tokens -------------------------------------------------------------------------------
+
+namespace {
+
+int check_chunk(const rocketkv_chunk_t* ch, const char* who) {
+  if (!ch) return fail(ROCKETKV_INVALID_ARG, "%s: chunk is NULL", who);
+  if (!ch->starts) return fail(ROCKETKV_INVALID_ARG, "%s: chunk->starts must not be NULL", who);
+  if (ch->n_tokens < 0) return fail(ROCKETKV_INVALID_ARG, "%s: n_tokens must be >= 0", who);
+  if (ch->n_tokens > ROCKETKV_MAX_CHUNK)
+    return fail(ROCKETKV_UNSUPPORTED, "%s: n_tokens %d exceeds %d", who, ch->n_tokens, ROCKETKV_MAX_CHUNK);
+  return ROCKETKV_OK;
+}
+
+int check_rope(const rocketkv_rope_t* r, const char* who) {
+  if (!r) return fail(ROCKETKV_INVALID_ARG, "%s: rope is NULL", who);
+  if (r->rot_dim < 2 || r->rot_dim > kHeadDim || r->rot_dim % 2 != 0)
+    return fail(ROCKETKV_INVALID_ARG, "%s: rot_dim %d must be even and in [2, %d]", who, r->rot_dim, kHeadDim);
+  if (r->interleaved != 0 && r->interleaved != 1)
+    return fail(ROCKETKV_INVALID_ARG, "%s: interleaved must be 0 or 1", who);
+  if (!r->inv_freq) return fail(ROCKETKV_INVALID_ARG, "%s: inv_freq must not be NULL", who);
+  if ((uintptr_t)r->inv_freq & 7) return fail(ROCKETKV_INVALID_ARG, "%s: inv_freq must be 8-byte aligned", who);
+  return ROCKETKV_OK;
+}
+
+int check_rows(const void* p, int64_t stride, int n_heads, const char* what, const char* who) {
+  if (!p) return fail(ROCKETKV_INVALID_ARG, "%s: %s must not be NULL", who, what);
+  if ((uintptr_t)p & 15) return fail(ROCKETKV_INVALID_ARG, "%s: %s must be 16-byte aligned", who, what);
+  if (stride < (int64_t)n_heads * kHeadDim || stride % 8 != 0)
+    return fail(ROCKETKV_INVALID_ARG, "%s: the stride of %s must be a multiple of 8 and at least %d heads", who, what, n_heads);
+  return ROCKETKV_OK;
+}
+
+int check_workspace(const void* ws, size_t have, size_t need, const char* who) {
+  if (need && (!ws || have < need))
+    return fail(ROCKETKV_WORKSPACE_TOO_SMALL, "%s: workspace %zu bytes < %zu needed", who, ws ? have : (size_t)0, need);
+  if ((uintptr_t)ws & 255) return fail(ROCKETKV_INVALID_ARG, "%s: workspace must be 256-byte aligned", who);
+  return ROCKETKV_OK;
+}
+
+RopeView rope_of(const rocketkv_rope_t* r) {
+  RopeView v = {0, 0, nullptr, 1.f};
+  if (r) v = {r->rot_dim, r->interleaved, r->inv_freq, r->scale};
+  return v;
+}
+
+ChunkView chunk_of(const rocketkv_chunk_t* ch) { return {ch->n_tokens, ch->starts}; }
+
+}  // namespace
+
+extern "C" {
+
+int32_t rocketkv_rope_frequencies(int32_t kind, int32_t rot_dim, double theta, double factor, double low, double high,
+                                  int64_t original, double* inv_freq, float* scale) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_rope_frequencies";
+  if (!inv_freq || !scale) return fail(ROCKETKV_INVALID_ARG, "%s: inv_freq / scale must not be NULL", who);
+  if (kind < ROCKETKV_ROPE_PLAIN || kind > ROCKETKV_ROPE_RAMP) return fail(ROCKETKV_INVALID_ARG, "%s: unknown kind %d", who, kind);
+  if (rot_dim < 2 || rot_dim > kHeadDim || rot_dim % 2 != 0)
+    return fail(ROCKETKV_INVALID_ARG, "%s: rot_dim %d must be even and in [2, %d]", who, rot_dim, kHeadDim);
+  if (!(theta > 1.0) || !isfinite(theta)) return fail(ROCKETKV_INVALID_ARG, "%s: theta must be finite and exceed 1", who);
+  if (kind != ROCKETKV_ROPE_PLAIN && (!(factor >= 1.0) || !isfinite(factor)))
+    return fail(ROCKETKV_INVALID_ARG, "%s: factor must be finite and at least 1", who);
+  if (kind == ROCKETKV_ROPE_BASE && rot_dim < 4) return fail(ROCKETKV_INVALID_ARG, "%s: BASE needs rot_dim > 2", who);
+  const bool mixes = kind == ROCKETKV_ROPE_BANDS || kind == ROCKETKV_ROPE_RAMP;
+  if (mixes && (!(low > 0.0) || !(high > low) || !isfinite(high) || original < 1))
+    return fail(ROCKETKV_INVALID_ARG, "%s: need 0 < low < high and original >= 1", who);
+  const double two_pi = 6.283185307179586476925;
+  const double base = kind == ROCKETKV_ROPE_BASE ? theta * pow(factor, (double)rot_dim / (rot_dim - 2)) : theta;
+  // index at which a frequency makes `turns` turns over the original context
+  const auto index_of = [&](double turns) { return 0.5 * rot_dim * log((double)original / (turns * two_pi)) / log(theta); };
+  double a = 0.0, b = 0.0;
+  if (kind == ROCKETKV_ROPE_RAMP) {
+    a = fmin(fmax(floor(index_of(high)), 0.0), rot_dim - 1.0);
+    b = fmin(fmax(ceil(index_of(low)), 0.0), rot_dim - 1.0);
+    if (b < a + 0.001) b = a + 0.001;
+  }
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    const double f = pow(base, -2.0 * i / rot_dim);
+    double u = 1.0;  // share of the unstretched frequency
+    if (kind == ROCKETKV_ROPE_LINEAR) u = 0.0;
+    if (kind == ROCKETKV_ROPE_BANDS) u = fmin(fmax(((double)original * f / two_pi - low) / (high - low), 0.0), 1.0);
+    if (kind == ROCKETKV_ROPE_RAMP) u = 1.0 - fmin(fmax((i - a) / (b - a), 0.0), 1.0);
+    inv_freq[i] = u == 1.0 ? f : (1.0 - u) * f / factor + u * f;
+  }
+  *scale = kind == ROCKETKV_ROPE_RAMP ? (float)(0.1 * log(factor) + 1.0) : 1.f;
+  return ROCKETKV_OK;
+}
+
+int32_t rocketkv_rope(const rocketkv_rope_t* rope, const int32_t* positions, int32_t n_tokens, int32_t n_heads,
+                      const void* x, int64_t x_stride, void* y, int64_t y_stride, void* stream) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_rope";
+  if (int r = check_rope(rope, who)) return r;
+  if (n_tokens < 0 || n_heads < 1) return fail(ROCKETKV_INVALID_ARG, "%s: need n_tokens >= 0 and n_heads >= 1", who);
+  if (n_tokens > ROCKETKV_MAX_CHUNK || n_heads > 4096)
+    return fail(ROCKETKV_UNSUPPORTED, "%s: more than %d tokens or 4096 heads", who, ROCKETKV_MAX_CHUNK);
+  if (!positions) return fail(ROCKETKV_INVALID_ARG, "%s: positions must not be NULL", who);
+  if (int r = check_rows(x, x_stride, n_heads, "x", who)) return r;
+  if (int r = check_rows(y, y_stride, n_heads, "y", who)) return r;
+  if (x == y && x_stride != y_stride) return fail(ROCKETKV_INVALID_ARG, "%s: in place needs equal strides", who);
+  const hipError_t e = launch_rope(rope_of(rope), positions, n_tokens, n_heads, static_cast<const bf16_t*>(x), x_stride,
+                                   static_cast<bf16_t*>(y), y_stride, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
+}
+
+int32_t rocketkv_append_chunk(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const rocketkv_rope_t* rope,
+                              const int32_t* positions, const void* q, int64_t q_stride, void* q_out, const void* k_new,
+                              int64_t k_stride, const void* v_new, int64_t v_stride, void* kmax, void* kmin,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_append_chunk";
+  if (int r = check_cache(cache, true, who)) return r;
+  if (int r = check_attend_shape(cache, who)) return r;
+  if (int r = check_chunk(chunk, who)) return r;
+  if (rope)
+    if (int r = check_rope(rope, who)) return r;
+  if (positions && !rope) return fail(ROCKETKV_INVALID_ARG, "%s: positions without rope", who);
+  if (!q != !q_out) return fail(ROCKETKV_INVALID_ARG, "%s: q and q_out go together", who);
+  if (q) {
+    if (int r = check_rows(q, q_stride, cache->n_q_heads, "q", who)) return r;
+    if (int r = check_rows(q_out, (int64_t)cache->n_q_heads * kHeadDim, cache->n_q_heads, "q_out", who)) return r;
+    if (q == q_out && q_stride != (int64_t)cache->n_q_heads * kHeadDim)
+      return fail(ROCKETKV_INVALID_ARG, "%s: in place needs equal strides", who);
+  }
+  if (int r = check_rows(k_new, k_stride, cache->n_kv_heads, "k_new", who)) return r;
+  if (int r = check_rows(v_new, v_stride, cache->n_kv_heads, "v_new", who)) return r;
+  if (!kmax != !kmin) return fail(ROCKETKV_INVALID_ARG, "%s: kmax and kmin go together", who);
+  if (((uintptr_t)kmax | (uintptr_t)kmin) & 15)
+    return fail(ROCKETKV_INVALID_ARG, "%s: kmax / kmin must be 16-byte aligned", who);
+  if (int r = check_workspace(workspace, workspace_bytes, ROCKETKV_WS_HEADER_BYTES, who)) return r;
+  const hipError_t e = launch_append_chunk(
+      view_of(cache), chunk_of(chunk), rope_of(rope), positions, static_cast<const bf16_t*>(q), q_stride,
+      static_cast<bf16_t*>(q_out), static_cast<const bf16_t*>(k_new), k_stride, static_cast<const bf16_t*>(v_new), v_stride,
+      static_cast<bf16_t*>(kmax), static_cast<bf16_t*>(kmin), workspace, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
+}
+
+int32_t rocketkv_chunk_attend(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const void* q, void* out,
+                              float* out_lse, void* workspace, size_t workspace_bytes, void* stream) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_chunk_attend";
+  if (int r = check_cache(cache, true, who)) return r;
+  if (int r = check_attend_shape(cache, who)) return r;
+  if (int r = check_chunk(chunk, who)) return r;
+  const int64_t stride = (int64_t)cache->n_q_heads * kHeadDim;
+  if (int r = check_rows(q, stride, cache->n_q_heads, "q", who)) return r;
+  if (int r = check_rows(out, stride, cache->n_q_heads, "out", who)) return r;
+  const CacheView v = view_of(cache);
+  const ChunkPlan plan = plan_chunk_attend(v, chunk->n_tokens);
+  if (plan.workgroups > 2147483647ll) return fail(ROCKETKV_UNSUPPORTED, "%s: too many rows for one launch", who);
+  if (int r = check_workspace(workspace, workspace_bytes, plan.total_bytes, who)) return r;
+  const hipError_t e = launch_chunk_attend(v, chunk_of(chunk), static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out),
+                                           out_lse, workspace, plan, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
+}
+
+int32_t rocketkv_accumulate_weights(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const void* q,
+                                    const float* lse, const float* weights_in, float* weights_out, void* stream) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_accumulate_weights";
+  if (int r = check_cache(cache, true, who)) return r;
+  if (int r = check_chunk(chunk, who)) return r;
+  if (!weights_out) return fail(ROCKETKV_INVALID_ARG, "%s: weights_out must not be NULL", who);
+  if (chunk->n_tokens > 0) {
+    if (int r = check_rows(q, (int64_t)cache->n_q_heads * kHeadDim, cache->n_q_heads, "q", who)) return r;
+    if (!lse) return fail(ROCKETKV_INVALID_ARG, "%s: lse must not be NULL", who);
+  }
+  const hipError_t e = launch_weights(view_of(cache), chunk_of(chunk), static_cast<const bf16_t*>(q), lse, weights_in,
+                                      weights_out, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
+}
+
+int32_t rocketkv_weight_evict(const rocketkv_cache_t* src, const float* weights, int32_t n_recent, int32_t keep_budget,
+                              const rocketkv_cache_t* dst, float* dst_weights, int32_t* kept_idx, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_weight_evict";
+  if (int r = check_cache(src, true, who)) return r;
+  if (int r = check_cache(dst, true, who)) return r;
+  if (int r = check_attend_shape(src, who)) return r;
+  if (int r = check_attend_shape(dst, who)) return r;
+  if (!weights) return fail(ROCKETKV_INVALID_ARG, "%s: weights must not be NULL", who);
+  if (keep_budget < 1 || n_recent < 0 || n_recent > keep_budget)
+    return fail(ROCKETKV_INVALID_ARG, "%s: need 0 <= n_recent (%d) <= keep_budget (%d), keep_budget >= 1", who, n_recent, keep_budget);
+  if (src->batch != dst->batch || src->n_q_heads != dst->n_q_heads || src->n_kv_heads != dst->n_kv_heads)
+    return fail(ROCKETKV_INVALID_ARG, "%s: src and dst must agree on batch and head counts", who);
+  if ((int64_t)dst->pages_cap * dst->page_size < keep_budget)
+    return fail(ROCKETKV_INVALID_ARG, "%s: dst holds %lld tokens per sequence < keep_budget %d", who,
+                (long long)dst->pages_cap * dst->page_size, keep_budget);
+  if (src->k_pool == dst->k_pool || src->v_pool == dst->v_pool || src->seq_lens == dst->seq_lens)
+    return fail(ROCKETKV_INVALID_ARG, "%s: src and dst pools and lengths must be distinct", who);
+  if (weights == dst_weights) return fail(ROCKETKV_INVALID_ARG, "%s: weights and dst_weights must be distinct", who);
+  const CacheView sv = view_of(src), dv = view_of(dst);
+  const EvictPlan plan = plan_evict(sv, keep_budget);
+  if (int r = check_workspace(workspace, workspace_bytes, plan.total_bytes, who)) return r;
+  const hipError_t e = launch_evict(sv, weights, n_recent, keep_budget, dv, dst_weights, kept_idx, workspace, plan,
+                                    static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
 }
 
 }  // extern "C"

@@ -357,4 +357,69 @@ hipError_t launch_snapkv(const bf16_t* q_obs, const CacheView& src, int window, 
                          int keep, const CacheView* dst, int32_t* kept_idx, int kept_stride,
                          int32_t* n_out, void* ws, const SnapPlan& plan, hipStream_t st);
 
+// ---- a chunk of new tokens ----
+struct ChunkView {
+  int32_t n_tokens;
+  const int32_t* starts;  // [batch + 1]
+};
+// First row and number of rows of sequence b, whatever `starts` holds.
+__device__ __forceinline__ int chunk_first(const ChunkView& ch, int b) { return min(max(ch.starts[b], 0), ch.n_tokens); }
+__device__ __forceinline__ int chunk_rows(const ChunkView& ch, int b) {
+  return max(0, min(ch.starts[b + 1], ch.n_tokens) - chunk_first(ch, b));
+}
+// The sequences bring `count(b)` pieces of work each: which one is piece `at` of all, and its index there.  Every
+// wavefront finds out for itself, a sequence per lane.
+template <class Count>
+__device__ __forceinline__ bool locate_tile(int batch, int at, const Count& count, int& b, int& idx) {
+  const int lane = threadIdx.x % kWave;
+  int before = 0;
+  for (int b0 = 0; b0 < batch; b0 += kWave) {
+    const int n = b0 + lane < batch ? count(b0 + lane) : 0;
+    const int upto = before + (int)wave_incl_scan((uint32_t)n);
+    const unsigned long long beyond = __ballot(upto > at);
+    if (beyond != 0ull) {
+      const int src = __ffsll(beyond) - 1;
+      b = b0 + src;
+      idx = at - (__builtin_amdgcn_readlane(upto, src) - __builtin_amdgcn_readlane(n, src));
+      return true;
+    }
+    before = __builtin_amdgcn_readlane(upto, kWave - 1);
+  }
+  return false;
+}
+
+struct RopeView {
+  int32_t rot_dim;  // 0: nothing is turned
+  int32_t interleaved;
+  const double* inv_freq;
+  float scale;
+};
+hipError_t launch_rope(const RopeView& r, const int32_t* positions, int n_tokens, int n_heads, const bf16_t* x,
+                       int64_t x_stride, bf16_t* y, int64_t y_stride, hipStream_t st);
+hipError_t launch_append_chunk(const CacheView& c, const ChunkView& ch, const RopeView& r, const int32_t* positions,
+                               const bf16_t* q, int64_t q_stride, bf16_t* q_out, const bf16_t* k, int64_t k_stride,
+                               const bf16_t* v, int64_t v_stride, bf16_t* kmax, bf16_t* kmin, void* ws, hipStream_t st);
+struct ChunkPlan {
+  int blocks;       // blocks of 32 rows to a wavefront
+  int tile_rows, tile_tokens;
+  int target;       // workgroups wanted where there are fewer tiles
+  bool cuts;        // there may be fewer
+  int64_t workgroups;
+  size_t total_bytes;
+};
+ChunkPlan plan_chunk_attend(const CacheView& c, int n_tokens);
+hipError_t launch_chunk_attend(const CacheView& c, const ChunkView& ch, const bf16_t* q, bf16_t* out, float* out_lse,
+                               void* ws, const ChunkPlan& plan, hipStream_t st);
+hipError_t launch_weights(const CacheView& c, const ChunkView& ch, const bf16_t* q, const float* lse, const float* w_in,
+                          float* w_out, hipStream_t st);
+struct EvictPlan {
+  int slices;     // histograms per row, 0: none are needed
+  int split;      // workgroups per row in the select
+  int slice_len;  // positions of each
+  size_t kept_off, hist_off, total_bytes;
+};
+EvictPlan plan_evict(const CacheView& src, int keep);
+hipError_t launch_evict(const CacheView& src, const float* weights, int n_recent, int keep, const CacheView& dst,
+                        float* dst_weights, int32_t* kept_idx, void* ws, const EvictPlan& plan, hipStream_t st);
+
 }  // namespace rkv

@@ -18,6 +18,9 @@ LIB_PATH = os.path.join(_HERE, "librocketkv.so")
 
 OK, INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP_ERROR = 0, -1, -2, -3, -4
 OP_HSA_DECODE, OP_DENSE_DECODE, OP_SNAPKV, OP_ATTEND = 0, 1, 2, 3
+OP_APPEND_CHUNK, OP_CHUNK_ATTEND, OP_WEIGHT_EVICT = 4, 5, 6
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3, 4
+MAX_CHUNK = 1 << 24
 MAX_PAGES = 32768
 V_CHANNEL_MAJOR, V_TOKEN_MAJOR = 0, 1
 
@@ -29,6 +32,8 @@ EXPORTS = [
     "rocketkv_mt_append_kv", "rocketkv_mt_hsa_decode_append",
     "rocketkv_stream_read", "rocketkv_stream_read_sink_bytes", "rocketkv_hsa_decode_noalloc",
     "rocketkv_stream_gather", "rocketkv_stream_gather_sink_bytes",
+    "rocketkv_rope_frequencies", "rocketkv_rope", "rocketkv_append_chunk", "rocketkv_chunk_attend",
+    "rocketkv_accumulate_weights", "rocketkv_weight_evict",
 ]
 NOALLOC_SCRATCH_BYTES = 4 << 20
 
@@ -54,6 +59,16 @@ class IndexStruct(C.Structure):
     """Mirror of ``rocketkv_index_t``."""
     _fields_ = [("token_index", C.c_void_p), ("n_indexed", C.c_void_p), ("page_size", C.c_int32),
                 ("pages_cap", C.c_int32)]
+
+
+class ChunkStruct(C.Structure):
+    """Mirror of ``rocketkv_chunk_t``."""
+    _fields_ = [("n_tokens", C.c_int32), ("starts", C.c_void_p)]
+
+
+class RopeStruct(C.Structure):
+    """Mirror of ``rocketkv_rope_t``."""
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("inv_freq", C.c_void_p), ("scale", C.c_float)]
 
 
 class SplitStruct(C.Structure):
@@ -121,6 +136,19 @@ def lib():
         L.rocketkv_mt_append_kv.argtypes = [cp, ip, vp, vp, vp, vp, vp]
         L.rocketkv_mt_hsa_decode_append.restype = i32
         L.rocketkv_mt_hsa_decode_append.argtypes = [cp, ip, vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+        hp, rp, i64, dbl = C.POINTER(ChunkStruct), C.POINTER(RopeStruct), C.c_int64, C.c_double
+        L.rocketkv_rope_frequencies.restype = i32
+        L.rocketkv_rope_frequencies.argtypes = [i32, i32, dbl, dbl, dbl, dbl, i64, C.POINTER(dbl), C.POINTER(C.c_float)]
+        L.rocketkv_rope.restype = i32
+        L.rocketkv_rope.argtypes = [rp, vp, i32, i32, vp, i64, vp, i64, vp]
+        L.rocketkv_append_chunk.restype = i32
+        L.rocketkv_append_chunk.argtypes = [cp, hp, rp, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+        L.rocketkv_chunk_attend.restype = i32
+        L.rocketkv_chunk_attend.argtypes = [cp, hp, vp, vp, vp, vp, sz, vp]
+        L.rocketkv_accumulate_weights.restype = i32
+        L.rocketkv_accumulate_weights.argtypes = [cp, hp, vp, vp, vp, vp, vp]
+        L.rocketkv_weight_evict.restype = i32
+        L.rocketkv_weight_evict.argtypes = [cp, vp, i32, i32, cp, vp, vp, vp, sz, vp]
         L.rocketkv_decompose.restype = i32
         L.rocketkv_decompose.argtypes = [C.c_int64, i32, i32, C.POINTER(SplitStruct)]
         L.rocketkv_last_error.restype = C.c_char_p
@@ -435,6 +463,149 @@ def mt_hsa_decode_append(cache: Cache, index: Index, q, k_new, v_new, kmax, kmin
                                                n_recent_pages, _ptr(out), _ptr(out_lse), _ptr(out_pages),
                                                _ptr(out_channels), _ptr(workspace), workspace.numel(),
                                                _stream(stream)))
+
+
+@dataclass
+class Chunk:
+    """The new tokens of all sequences of a cache, packed: rows starts[b] .. starts[b+1]-1 are sequence b's.
+
+    starts: int32 [batch + 1] on the device; n_tokens: rows of the packed tensors."""
+    starts: object
+    n_tokens: int
+
+    def struct(self, cache: Cache) -> ChunkStruct:
+        _tensor("starts", self.starts, "int32", (cache.batch + 1,))
+        return ChunkStruct(self.n_tokens, _ptr(self.starts))
+
+
+@dataclass
+class Rope:
+    """Rotary positions: inv_freq, float64 [rot_dim / 2] on the device, in radians per position (see rope_frequencies)."""
+    inv_freq: object
+    interleaved: bool = False
+    scale: float = 1.0
+
+    def struct(self) -> RopeStruct:
+        _tensor("inv_freq", self.inv_freq, "float64", (None,))
+        return RopeStruct(2 * int(self.inv_freq.shape[0]), int(self.interleaved), _ptr(self.inv_freq), self.scale)
+
+
+def _tensor(name, t, dtype, shape, rows=False):
+    """What a pointer cannot say: type, shape (None: any) and layout, contiguous or, with `rows`, in rows of any stride."""
+    import torch
+    ok = t.dtype == getattr(torch, dtype) and t.dim() == len(shape) and all(s in (None, n) for s, n in zip(shape, t.shape))
+    if not ok:
+        raise RocketKVError(INVALID_ARG, f"{name}: need {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if not (t.is_contiguous() or (rows and t.numel() > 0 and t[0].is_contiguous())):
+        raise RocketKVError(INVALID_ARG, f"{name}: inner dimensions must be contiguous")
+
+
+def _row_stride(t):
+    """Elements between tokens (a single token may have any)."""
+    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1] * t.shape[2])
+
+
+def rope_frequencies(rot_dim: int, theta: float, kind: int = ROPE_PLAIN, factor: float = 1.0, low: float = 1.0,
+                     high: float = 4.0, original: int = 8192, device=None, interleaved: bool = False) -> Rope:
+    """Rotary positions with (stretched) frequencies (host arithmetic in the library); see rocketkv_rope_frequencies."""
+    import torch
+    if rot_dim < 0:
+        raise RocketKVError(INVALID_ARG, f"rot_dim {rot_dim} must not be negative")
+    freq, scale = (C.c_double * max(rot_dim // 2, 1))(), C.c_float()
+    _check(lib().rocketkv_rope_frequencies(kind, rot_dim, theta, factor, low, high, original, freq, C.byref(scale)))
+    return Rope(torch.tensor(list(freq), dtype=torch.float64, device=device), interleaved, scale.value)
+
+
+def rope(rope: Rope, positions, x, y, stream=None):
+    """x, y: bf16 [tokens][heads][128], tokens at any stride; positions: int32 [tokens].  y may be x."""
+    n, heads = int(x.shape[0]), int(x.shape[1])
+    _tensor("x", x, "bfloat16", (None, None, 128), rows=True)
+    _tensor("y", y, "bfloat16", (n, heads, 128), rows=True)
+    _tensor("positions", positions, "int32", (n,))
+    if n == 0:
+        return
+    r = rope.struct()
+    _check(lib().rocketkv_rope(C.byref(r), _ptr(positions), n, heads, _ptr(x), _row_stride(x), _ptr(y), _row_stride(y),
+                               _stream(stream)))
+
+
+def append_chunk(cache: Cache, chunk: Chunk, k_new, v_new, kmax, kmin, workspace, rope: Optional[Rope] = None,
+                 positions=None, q=None, q_out=None, stream=None):
+    """k_new, v_new: bf16 [n_tokens][n_kv_heads][128], q: bf16 [n_tokens][n_q_heads][128], tokens at any stride."""
+    n = chunk.n_tokens
+    for name, t, heads in (("k_new", k_new, cache.n_kv_heads), ("v_new", v_new, cache.n_kv_heads), ("q", q, cache.n_q_heads)):
+        if t is not None:
+            _tensor(name, t, "bfloat16", (n, heads, 128), rows=True)
+    if q_out is not None:
+        _tensor("q_out", q_out, "bfloat16", (n, cache.n_q_heads, 128))
+    if positions is not None:
+        _tensor("positions", positions, "int32", (n,))
+    _summaries(cache, kmax, kmin)
+    if n == 0:
+        return
+    st, ch, r = cache.struct(), chunk.struct(cache), rope.struct() if rope is not None else None
+    stride = lambda t: 0 if t is None else _row_stride(t)
+    _check(lib().rocketkv_append_chunk(C.byref(st), C.byref(ch), C.byref(r) if r is not None else None, _ptr(positions),
+                                       _ptr(q), stride(q), _ptr(q_out), _ptr(k_new), stride(k_new), _ptr(v_new),
+                                       stride(v_new), _ptr(kmax), _ptr(kmin), _ptr(workspace), workspace.numel(),
+                                       _stream(stream)))
+
+
+def _summaries(cache, kmax, kmin):
+    for name, t in (("kmax", kmax), ("kmin", kmin)):
+        if t is not None:
+            _tensor(name, t, "bfloat16", (cache.batch, cache.n_kv_heads, cache.head_dim, cache.pages_cap))
+
+
+def chunk_attend(cache: Cache, chunk: Chunk, q, out, out_lse, workspace, stream=None):
+    """q, out: bf16 [n_tokens][n_q_heads][128]; out_lse: float32 [n_tokens][n_q_heads] or None."""
+    n = chunk.n_tokens
+    _tensor("q", q, "bfloat16", (n, cache.n_q_heads, 128))
+    _tensor("out", out, "bfloat16", (n, cache.n_q_heads, 128))
+    if out_lse is not None:
+        _tensor("out_lse", out_lse, "float32", (n, cache.n_q_heads))
+    if n == 0:
+        return
+    st, ch = cache.struct(), chunk.struct(cache)
+    _check(lib().rocketkv_chunk_attend(C.byref(st), C.byref(ch), _ptr(q), _ptr(out), _ptr(out_lse), _ptr(workspace),
+                                       workspace.numel(), _stream(stream)))
+
+
+def alloc_weights(cache: Cache):
+    """Zeroed accumulated weights of a cache."""
+    import torch
+    return torch.zeros((cache.batch, cache.n_kv_heads, cache.pages_cap * cache.page_size), dtype=torch.float32,
+                       device=cache.k_pool.device)
+
+
+def _weights(name, t, cache):
+    _tensor(name, t, "float32", (cache.batch, cache.n_kv_heads, cache.pages_cap * cache.page_size))
+
+
+def accumulate_weights(cache: Cache, chunk: Chunk, q, lse, weights_in, weights_out, stream=None):
+    """q: bf16 [n_tokens][n_q_heads][128], lse: float32 [n_tokens][n_q_heads]; weights as of alloc_weights, weights_in
+    None or weights_out itself if it is to be added to."""
+    n = chunk.n_tokens
+    _tensor("q", q, "bfloat16", (n, cache.n_q_heads, 128))
+    _tensor("lse", lse, "float32", (n, cache.n_q_heads))
+    if weights_in is not None:
+        _weights("weights_in", weights_in, cache)
+    _weights("weights_out", weights_out, cache)
+    st, ch = cache.struct(), chunk.struct(cache)
+    _check(lib().rocketkv_accumulate_weights(C.byref(st), C.byref(ch), _ptr(q), _ptr(lse), _ptr(weights_in),
+                                             _ptr(weights_out), _stream(stream)))
+
+
+def weight_evict(src: Cache, weights, n_recent: int, keep_budget: int, dst: Cache, dst_weights, kept_idx, workspace,
+                 stream=None):
+    _weights("weights", weights, src)
+    if dst_weights is not None:
+        _weights("dst_weights", dst_weights, dst)
+    if kept_idx is not None:
+        _tensor("kept_idx", kept_idx, "int32", (src.batch, src.n_kv_heads, keep_budget))
+    s, d = src.struct(), dst.struct()
+    _check(lib().rocketkv_weight_evict(C.byref(s), _ptr(weights), n_recent, keep_budget, C.byref(d), _ptr(dst_weights),
+                                       _ptr(kept_idx), _ptr(workspace), workspace.numel(), _stream(stream)))
 
 
 def decompose(seq_len: int, token_budget: int, head_dim: int = 128) -> dict:
