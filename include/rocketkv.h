@@ -425,7 +425,7 @@ int32_t rocketkv_append_chunk(const rocketkv_cache_t* cache, const rocketkv_chun
  * bf16 result.  Whole prompts (seq_lens[b] == n), pieces of prompts, turns and single tokens mix freely.
  * q, out: bf16 [n_tokens][n_q_heads][head_dim].  out_lse: optional fp32 [n_tokens][n_q_heads], natural-log sum-exp of the
  * scaled logits.  Absent pages are skipped; a row with nothing to attend to gets zeros and -inf.
- * A cached value of a row's future that is not finite reaches the rows of its own chunk that share its 64 tokens.
+ * Keys and values of a row's future, and whatever lies where no token is, may be anything.
  * workspace: rocketkv_workspace_bytes(ROCKETKV_OP_CHUNK_ATTEND, cache, n_tokens, 0).
  */
 int32_t rocketkv_chunk_attend(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const void* q, void* out,

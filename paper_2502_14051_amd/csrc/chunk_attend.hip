@@ -13,6 +13,8 @@
 // product leaves a lane the keys of A's rows 8a + 4h + r; with the rows of K read in an order that swaps bits 2 and 3,
 // these are keys 16x + 8h + 0..7, which packed to bf16 are the second product's operand as they stand.  P is rounded to
 // bf16 there (relative 2^-9 at most each, the sum l takes the unrounded values); everything else is fp32.
+#include <type_traits>
+
 #include "attend_core.h"
 #include "chunk_division.h"
 
@@ -25,20 +27,27 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = 64;                                        // keys per step
 constexpr int kKeyBytes = kStep * kHeadDim * (int)sizeof(bf16_t);  // keys (and values) of a step
-constexpr int kChunkT = 256;
-constexpr int kRowStride = kHeadDim + 2;  // a row of a part: O[128], maximum, sum
-constexpr float kLazy = 8.f;              // a maximum may be exceeded by a factor of 2^8 before sums are scaled anew
+constexpr float kSumLimit = 65536.f;      // of 16 exponentials, beyond which the maximum is looked at
+constexpr float kLazy = 8.f;              // and followed where it has grown by 2^8
 
-// 16 bytes per lane from `src` straight to LDS: lane l's land 16 l bytes behind the wavefront's `dst`
-__device__ __forceinline__ void to_lds(const bf16_t* src, unsigned char* dst) {
+// 16 bytes per lane straight to LDS: lane l's land 16 l bytes behind the wavefront's `dst`.  From a base that is the same
+// for the wavefront and 32 bits of offset a lane; to_lds_far from any address.  (After loads of the second kind the compiler
+// takes every wait for LDS to be a wait for all of LDS, as it does for accesses through generic pointers.)
+__device__ __forceinline__ void to_lds(const void* base, uint32_t bytes, uint32_t off, unsigned char* dst) {
+#ifdef __HIP_DEVICE_COMPILE__
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00020000),
+                                           (__attribute__((address_space(3))) void*)dst, 16, (int)off, 0, 0, 0);
+#endif
+}
+__device__ __forceinline__ void to_lds_far(const void* src, unsigned char* dst) {
 #ifdef __HIP_DEVICE_COMPILE__
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
                                    (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 #endif
 }
 
-// Four bf16 of a column each: the 16 lanes of a row name 16 pieces of four neighbours, four rows of four pieces; lane i
-// gets element i % 4 + 4 ... of the transposed block: column i of the 16, rows 0..3.
+// A 4 x 16 block of bf16 by columns: of the 16 lanes of a row, lane i names four neighbours, piece i % 4 of block row i / 4,
+// and gets column i of the block.
 __device__ __forceinline__ u32x2 lds_columns(const unsigned char* at) {
 #ifdef __HIP_DEVICE_COMPILE__
   const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
@@ -48,6 +57,24 @@ __device__ __forceinline__ u32x2 lds_columns(const unsigned char* at) {
 #endif
 }
 
+// Largest of 16 products times `c`, over both halves of the wavefront.  (v_max3 without the canonicalisation that fmaxf
+// brings along.  In front of assembly the compiler leaves no time for products to reach their registers; it does in front
+// of the multiplication, and the empty assembly puts the rest behind it.)
+__device__ __forceinline__ float top16(f32x16& s, float c) {
+  const auto max3 = [](float x, float y, float z) {
+    float d;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(d) : "v"(x), "v"(y), "v"(z));
+    return d;
+  };
+  const float last = s[15] * c;
+  asm volatile("" : "+v"(s) : "v"(last));
+  const float a = max3(s[0], s[1], s[2]), b = max3(s[3], s[4], s[5]), d = max3(s[6], s[7], s[8]);
+  const float e = max3(s[9], s[10], s[11]), f = max3(s[12], s[13], s[14]);
+  const float mine = fmaxf(max3(max3(a, b, d), e, f) * c, last);
+  const SwapPair sw = swap_rows32(__float_as_uint(mine));
+  return fmaxf(__uint_as_float(sw.a), __uint_as_float(sw.b));
+}
+
 }  // namespace
 
 struct ChunkAttendArgs {
@@ -55,9 +82,10 @@ struct ChunkAttendArgs {
   const bf16_t* q;
   bf16_t* out;
   float* out_lse;
-  float* partial;     // [workgroup][rows][kRowStride]; null: no tile is ever cut
+  float* partial;     // [workgroup][rows][128] sums of the parts; null: no tile is ever cut
+  float2* part_stats; // [workgroup][rows] their maxima and sums of exponentials
   int tile_tokens;    // tokens of a row tile
-  int target;         // workgroups wanted where there are fewer tiles
+  int slots;          // workgroups the chip holds at a time
 };
 
 // Where a workgroup works: tile `tile` of sequence b, part `part` of `parts` of its keys.
@@ -82,31 +110,28 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const CacheView& c, const ChunkVie
 __device__ __forceinline__ int chunk_size_for(const CacheView& c, const ChunkAttendArgs& a) {
   const int lane = threadIdx.x % kWave;
   if (!a.partial) return kChunkWhole;
-  int64_t work = 0, tiles = 0;
-  int longest = 0;
   const auto total = [](int x) { return __builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)x), kWave - 1); };
-  for (int b0 = 0; b0 < c.batch; b0 += kWave) {
-    int t = 0, steps = 0;
-    if (b0 + lane < c.batch) {
-      const ChunkSeq s = chunk_seq(c, a.ch, b0 + lane);
-      t = chunk_ceil(s.n, a.tile_tokens);
-      steps = t ? chunk_ceil(s.len, kStep) : 0;
-    }
-    tiles += total(t);
-    // (tiles are fewer than `target` where this counts, so that products of the sums stay far below 2^31)
-    work += (int64_t)total(min(t, a.target) * min(steps, (1 << 30) / a.target / kWave));
-    longest = max(longest, (int)wave_max_u32((uint32_t)steps));
-  }
-  return chunk_part_size(tiles * c.n_kv_heads, work * c.n_kv_heads, a.target, longest, [&](int size) {
-    int64_t n = 0;
+  ChunkLoad load = {0, 0.f, 0};
+  const auto each = [&](const auto& fn) {  // of the tiles and steps of every sequence
     for (int b0 = 0; b0 < c.batch; b0 += kWave) {
-      int x = 0;
+      int t = 0, steps = 0;
       if (b0 + lane < c.batch) {
         const ChunkSeq s = chunk_seq(c, a.ch, b0 + lane);
-        x = chunk_ceil(s.n, a.tile_tokens) * chunk_parts(chunk_ceil(s.len, kStep), size);
+        t = chunk_ceil(s.n, a.tile_tokens);
+        steps = t ? chunk_ceil(s.len, kStep) : 0;
       }
-      n += total(x);
+      fn(t, steps);
     }
+  };
+  each([&](int t, int steps) {
+    load.tiles += total(t) * c.n_kv_heads;
+    // (a coarser count keeps the sums in range where sequences are long: 2^15 steps are 2^21 tokens)
+    load.work += (float)total(min(t, a.slots * kChunkRounds) * min(steps, 1 << 15)) * (float)c.n_kv_heads;
+    load.longest = max(load.longest, (int)wave_max_u32((uint32_t)steps));
+  });
+  return chunk_part_size(load, a.slots, [&](int size) {
+    int n = 0;
+    each([&](int t, int steps) { n += total(t * chunk_parts(steps, size)); });
     return n * c.n_kv_heads;
   });
 }
@@ -127,216 +152,204 @@ __device__ __forceinline__ bool chunk_place(const CacheView& c, const ChunkAtten
   return true;
 }
 
-template <bool TOK, int NB>
-__global__ __launch_bounds__(kChunkT) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 2 : 1)))
+template <bool TOK, bool FAR, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave) __attribute__((amdgpu_waves_per_eu(2)))
 void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
-  extern __shared__ __align__(16) unsigned char s_tiles[];  // [2][keys, values]
-  __shared__ __align__(8) uint16_t s_valid[2][kStep / 16];  // the step's tokens that exist
-  constexpr int kRows = 4 * 32 * NB;
+  constexpr int kWaveTok = kStep / WAVES;  // tokens a wavefront brings
+  extern __shared__ __align__(256) unsigned char s_tiles[];          // [2] keys, [2] values
+  constexpr int kRows = WAVES * 32;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int col = lane % 32, h = lane / 32;
   const int g = blockIdx.x % c.n_kv_heads, at = blockIdx.x / c.n_kv_heads;
   ChunkPlace pl;
   if (!chunk_place(c, a, chunk_size_for(c, a), at, pl)) return;
-  if (pl.parts > 1 && (int)blockIdx.x >= a.target) return;  // (`starts` that overlap: no place for its rows)
+  if (pl.parts > 1 && (int)blockIdx.x >= a.slots * kChunkRounds) return;  // (`starts` that overlap: no place for its rows)
   const ChunkSeq s = chunk_seq(c, a.ch, pl.b);
   const int G = c.group, ps = c.page_size;
   const int t0 = pl.tile * a.tile_tokens, nt = min(a.tile_tokens, s.n - t0);
   const int rows = nt * G;
-  const int64_t lane_row0 = s.row + t0;
   const int pos0 = s.len - s.n + t0;  // place in the cache of the tile's first token
 
   // the part's steps
   const int steps = chunk_ceil(max(0, min(s.len, pos0 + nt)), kStep), per = chunk_ceil(steps, pl.parts);
   const int it0 = min(pl.part * per, steps), it1 = min(it0 + per, steps);
 
-  // this wavefront's rows: queries in registers, and the last key each row sees
-  bf16x8 qf[NB][8];
-  int last[NB], tok[NB], head[NB];
-  bool real[NB];
-#pragma unroll
-  for (int x = 0; x < NB; ++x) {
-    const int r = (wave * NB + x) * 32 + col;
-    real[x] = r < rows;
-    tok[x] = real[x] ? r / G : 0;
-    head[x] = real[x] ? r - tok[x] * G : 0;
-    last[x] = real[x] ? pos0 + tok[x] : -1;
-    const bf16_t* qp = a.q + ((lane_row0 + tok[x]) * c.n_q_heads + (int64_t)g * G + head[x]) * kHeadDim + h * 8;
+  // this lane's row: its query in registers, and the last key it sees
+  const int r = wave * 32 + col;
+  const bool working = wave * 32 < rows;
+  const int last = r < rows ? pos0 + r / G : -1;
+  const auto packed_row = [&](int r) {  // (token, head) of the packed tensors
+    const int t = r / G;
+    return (int64_t)(s.row + t0 + t) * c.n_q_heads + (int64_t)g * G + (r - t * G);
+  };
+  bf16x8 qf[8];
+  {
+    const bf16_t* qp = a.q + packed_row(min(r, rows - 1)) * kHeadDim + h * 8;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       u32x4 v = *reinterpret_cast<const u32x4*>(qp + j * 16);
-      if (!real[x]) v = (u32x4){0u, 0u, 0u, 0u};
-      qf[x][j] = as_bf16x8(v);
+      if (r >= rows) v = (u32x4){0u, 0u, 0u, 0u};
+      qf[j] = as_bf16x8(v);
     }
   }
-  const int wave_row0 = wave * NB * 32, wave_row1 = min(rows, wave_row0 + NB * 32) - 1;
-  const bool working = wave_row0 < rows;
-  const int sees_first = working ? pos0 + wave_row0 / G : -1;  // the last key that all of the wavefront's rows see
-  const int sees_last = working ? pos0 + wave_row1 / G : -1;   // and that any of them sees
+  const int sees_first = working ? pos0 + wave * 32 / G : -1;  // the last key that all of the wavefront's rows see
 
   // Keys and values of a step to LDS: every wavefront brings 16 tokens of each, 16 bytes a lane.
   //   keys: [64][16 chunks], chunk x of row r at x ^ r % 16, so that 32 rows at one chunk spread over the banks
-  //   values by channel: the four page tiles as they stand; by token: [64][16 chunks], chunk x of row r at x ^ 2 (r % 8)
-  const int64_t head_off = (int64_t)g * c.stride_head;
-  int page[4], slot[4], raw[4];  // TOK: page and slot of this lane's rows of the next step; else [0] only
+  //   values by channel: per page [8 blocks of 16 channels][2 halves of its tokens][16 channels], so that 16 lanes read 256
+  //   bytes in a row; by token: [64][16 chunks], chunk x of row r at x ^ 2 (r % 8)
+  constexpr int kLoads = kWaveTok / 4;        // of keys, and of values, a wavefront issues for a step: 1 KiB each
+  typedef typename std::conditional<TOK && !FAR, uint32_t, int64_t>::type Offset;  // bytes from the pool's beginning
+  const int first_tok = wave * kWaveTok;      // of the step
+  const int64_t head_off = (int64_t)g * c.stride_head * sizeof(bf16_t), page_off = c.stride_page * sizeof(bf16_t);
+  // Looked up a step ahead, by every wavefront for the whole step: lane i token i of it, or page i where pages are tiles.
+  int page = 0, slot = 0, raw = -1;
+  Offset off_k = 0, off_v = 0;  // where the step's rows lie: of the keys to be requested, of the values
+  const auto in_range = [&](int raw) { return raw >= 0 && (int64_t)raw < c.n_phys_pages; };
   const auto look_up = [&](int it) {
-    if (TOK) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int t = it * kStep + wave * 16 + 4 * j + lane / 16;
-        raw[j] = it < it1 && t < s.len ? phys_page_request(c, pl.b, page[j]) : -1;
-      }
-    } else {
-      const int p = it * (kStep / 16) + wave;
-      raw[0] = it < it1 && p * 16 < s.len ? phys_page_request(c, pl.b, p) : -1;
-    }
+    const int t0 = it * kStep, end = it < it1 ? s.len : 0;
+    if (TOK) raw = t0 + lane < end ? phys_page_request(c, pl.b, page) : -1;
+    else raw = lane < kStep / kAttnPage && t0 + lane * kAttnPage < end ? phys_page_request(c, pl.b, t0 / kAttnPage + lane) : -1;
   };
   if (TOK) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int t = it0 * kStep + wave * 16 + 4 * j + lane / 16;
-      page[j] = t / ps;
-      slot[j] = t - page[j] * ps;
-    }
+    page = (it0 * kStep + lane) / ps;
+    slot = it0 * kStep + lane - page * ps;
   }
   const int skip_pages = kStep / ps, skip_slots = kStep - skip_pages * ps;
-  const auto issue = [&](int it) {  // step `it`, looked up before; looks up the next one
-    unsigned char* kb = s_tiles + (it & 1) * 2 * kKeyBytes + wave * 16 * 256;
-    unsigned char* vb = kb + kKeyBytes;
-    if (TOK) {
-      uint32_t valid = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int64_t pp = phys_page_resolve(c, raw[j]);
-        const unsigned long long ok = __ballot(pp >= 0);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) valid |= (uint32_t)((ok >> (16 * x)) & 1u) << (4 * j + x);
-        const int64_t off = pp >= 0 ? pp * c.stride_page + head_off + slot[j] * kHeadDim : 0;
-        const int r = 4 * j + lane / 16;
-        to_lds(c.k_pool + off + ((lane % 16) ^ r) * 8, kb + j * 1024);
-        to_lds(c.v_pool + off + ((lane % 16) ^ 2 * (r % 8)) * 8, vb + j * 1024);
-        slot[j] += skip_slots;
-        page[j] += skip_pages;
-        if (slot[j] >= ps) { slot[j] -= ps; ++page[j]; }
-      }
-      if (lane == 0) s_valid[it & 1][wave] = (uint16_t)valid;
+  // 16 bytes a lane from the row of token `r` of the step, whose offset is with lane r
+  const auto row_to_lds = [&](const bf16_t* pool, Offset off, int r, int from, unsigned char* dst) {
+    const uint32_t lo = (uint32_t)__shfl((int)off, r);
+    if (FAR) {
+      const int64_t at = (int64_t)((uint64_t)(uint32_t)__shfl((int)((int64_t)off >> 32), r) << 32 | lo);
+      to_lds_far(reinterpret_cast<const char*>(pool) + at + from, dst);
     } else {
-      const int64_t pp = phys_page_resolve(c, raw[0]);
-      const int left = s.len - (it * kStep + wave * 16);
-      if (lane == 0) s_valid[it & 1][wave] = pp < 0 || left <= 0 ? 0 : left >= 16 ? 0xffffu : (uint16_t)((1u << left) - 1);
-      const int64_t off = pp >= 0 ? pp * c.stride_page + head_off : 0;
+      to_lds(pool, 0xffffffffu, lo + from, dst);
+    }
+  };
+  // Keys of step `it`, looked up before; looks up the next one.  Returns a bit per token of the step that exists.
+  const auto issue_keys = [&](int it, auto to) {
+    unsigned char* kb = s_tiles + decltype(to)::value * kKeyBytes + first_tok * 256;
+    unsigned long long valid = __ballot(in_range(raw));
+    if (TOK) {
+      off_k = in_range(raw) ? (Offset)(raw * page_off + head_off + slot * (kHeadDim * (int)sizeof(bf16_t))) : (Offset)0;
+      slot += skip_slots;
+      page += skip_pages;
+      if (slot >= ps) { slot -= ps; ++page; }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        to_lds(c.k_pool + off + (4 * j + lane / 16) * kHeadDim + ((lane % 16) ^ (4 * j + lane / 16)) * 8, kb + j * 1024);
-        to_lds(c.v_pool + off + j * 512 + lane * 8, vb + j * 1024);
+      for (int j = 0; j < kLoads; ++j) {  // 16 lanes a row
+        const int r = first_tok + 4 * j + lane / 16;
+        row_to_lds(c.k_pool, off_k, r, ((lane % 16) ^ r % 16) * 16, kb + j * 1024);
+      }
+    } else {
+      const int mine = __builtin_amdgcn_readlane(raw, first_tok / kAttnPage);
+      off_k = in_range(mine) ? (Offset)(mine * page_off + head_off) : (Offset)0;
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int r = first_tok % kAttnPage + 4 * j + lane / 16;
+        to_lds(reinterpret_cast<const char*>(c.k_pool) + off_k, 4096, r * 256 + ((lane % 16) ^ r) * 16, kb + j * 1024);
+      }
+      const int left = s.len - it * kStep;
+      if (valid == 0xfull && left >= kStep) {
+        valid = ~0ull;
+      } else {
+        unsigned long long tokens = 0;
+#pragma unroll
+        for (int x = 0; x < kStep / kAttnPage; ++x) tokens |= (valid >> x & 1ull) * 0xffffull << 16 * x;
+        valid = left >= kStep ? tokens : left > 0 ? tokens & ((1ull << left) - 1ull) : 0ull;
       }
     }
     look_up(it + 1);
+    return valid;
+  };
+  const auto issue_values = [&](auto to) {  // of the step whose offsets are in off_v
+    unsigned char* vb = s_tiles + (2 + decltype(to)::value) * kKeyBytes + first_tok * 256;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      if (TOK) {
+        const int r = first_tok + 4 * j + lane / 16;
+        row_to_lds(c.v_pool, off_v, r, ((lane % 16) ^ 2 * (r % 8)) * 16, vb + j * 1024);
+      } else {
+        to_lds(reinterpret_cast<const char*>(c.v_pool) + off_v, 4096,
+               (first_tok % kAttnPage / 4 + j) * 1024 + lane / 32 * 512 + lane % 16 * 32 + lane / 16 % 2 * 16, vb + j * 1024);
+      }
+    }
   };
 
-  f32x16 O[NB][4];
-  float m[NB], l[NB];
+  f32x16 O[4];
+  float m = kNegBig, l = 0.f;
 #pragma unroll
-  for (int x = 0; x < NB; ++x) {
-    m[x] = kNegBig;
-    l[x] = 0.f;
-#pragma unroll
-    for (int cb = 0; cb < 4; ++cb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) O[x][cb][i] = 0.f;
-  }
+  for (int cb = 0; cb < 4; ++cb) O[cb] = f32x16{};
   const float sc = kLog2e * 0.08838834764831845f;  // log2(e) / sqrt(128)
   // token of the tile whose keys this lane reads as row `col` of a product: bits 2 and 3 swapped
   const int key_row = (col & 0x13) | (col & 4) << 1 | (col & 8) >> 1;
 
-  const auto products = [&](const unsigned char* kb, int u, f32x16 (&S)[NB]) {
-    const unsigned char* row = kb + (u * 32 + key_row) * 256;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const bf16x8 kf = as_bf16x8(*reinterpret_cast<const u32x4*>(row + (((2 * j + h) ^ (key_row & 15)) * 16)));
-#pragma unroll
-      for (int x = 0; x < NB; ++x) {
-        const f32x16 zero = {};
-        S[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[x][j], j == 0 ? zero : S[x], 0, 0, 0);
-      }
-    }
+  // Chunk 2 j + h of this lane's row stands at (2 j + h) ^ key_row % 16.  `at`: key_at, kept from being turned into eight
+  // registers outside the loop.
+  const uint32_t key_at = (uint32_t)(key_row * 256 + (h ^ (key_row & 15)) * 16);
+  const auto read_key = [&](uint32_t at, auto slot, int u, int j, bf16x8& kf) {
+    kf = as_bf16x8(*reinterpret_cast<const u32x4*>(s_tiles + (at ^ (uint32_t)(32 * j)) + (decltype(slot)::value * kKeyBytes + u * 8192)));
   };
-  // channels 32 cb + col, tokens 32 u + 16 x + 8 h + 0..7
-  const auto value_part = [&](const unsigned char* vb, int u, int x, int cb) {
+  // Channels 32 cb + col, tokens 32 u + 16 y + 8 h + 0..7.  By token, lane i of a row of 16 names a piece of token row
+  // 4 z + i / 4 (z: first or second four) and of 16 channels; its chunk 4 cb + a stands at 4 cb ^ 8 z ^ (a ^ 2 (i / 4)), of
+  // which only bit 2 meets a bit of the lane's own: two addresses a lane, the rest is in the instruction.
+  const int vi = lane % 16, va = (2 * (lane / 16 % 2) + vi % 4 / 2) ^ (2 * (vi / 4));
+  const uint32_t value_at = TOK ? (uint32_t)((8 * h + vi / 4) * 256 + vi % 2 * 8 + va * 16) : (uint32_t)(col / 16 * 512 + h * 256 + col % 16 * 16);
+  const uint32_t value_at4 = value_at ^ 64u;
+  const auto read_value = [&](auto slot, int u, int y, int cb, u32x4& vf) {
+    const int base = (2 + decltype(slot)::value) * kKeyBytes + u * 8192;
     if (TOK) {
-      const int i = lane % 16, chunk = (32 * cb + 16 * (lane / 16 % 2)) / 8 + i % 4 / 2;
       u32x2 w[2];
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const int r = 32 * u + 16 * x + 8 * h + 4 * y + i / 4;
-        w[y] = lds_columns(vb + r * 256 + ((chunk ^ 2 * (r % 8)) * 16) + i % 2 * 8);
-      }
-      return (u32x4){w[0].x, w[0].y, w[1].x, w[1].y};
+      for (int z = 0; z < 2; ++z)
+        w[z] = lds_columns(s_tiles + (cb % 2 ? value_at4 : value_at) + (base + (16 * y + 4 * z) * 256 + ((cb / 2) ^ z) * 128));
+      vf = (u32x4){w[0].x, w[0].y, w[1].x, w[1].y};
+    } else {
+      vf = *reinterpret_cast<const u32x4*>(s_tiles + value_at + (base + y * 4096 + cb * 1024));
     }
-    return *reinterpret_cast<const u32x4*>(vb + (2 * u + x) * 4096 + (32 * cb + col) * 32 + h * 16);
   };
-
-  const auto unit = [&](const unsigned char* kb, const unsigned char* vb, int u, int key0, bool masked, uint32_t ok) {
-    f32x16 S[NB];
-    products(kb, u, S);
-    if (masked) {
+  const auto mask = [&](f32x16& S, int key0, uint32_t ok) {
+    const uint32_t there = ok >> (8 * h);
+    const int seen = last - key0 - 8 * h;
 #pragma unroll
-      for (int x = 0; x < NB; ++x)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int t = 16 * (i / 8) + 8 * h + i % 8;
-          if (!((ok >> t) & 1u) || key0 + t > last[x]) S[x][i] = -INFINITY;
-        }
+    for (int i = 0; i < 16; ++i) {
+      const int t = 16 * (i / 8) + i % 8;
+      if (!((there >> t) & 1u) || t > seen) S[i] = -INFINITY;
     }
-    u32x4 pf[NB][2];
-#pragma unroll
-    for (int x = 0; x < NB; ++x) {
-      float mx = S[x][0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, S[x][i]);
-      const SwapPair sw = swap_rows32(__float_as_uint(mx));
-      mx = fmaxf(__uint_as_float(sw.a), __uint_as_float(sw.b)) * sc;
-      if (__any(mx > m[x] + kLazy)) {
-        const float mn = mx > m[x] + kLazy ? mx : m[x];
-        const float alpha = fast_exp2(m[x] - mn);
-        m[x] = mn;
-        l[x] *= alpha;
-#pragma unroll
-        for (int cb = 0; cb < 4; ++cb) O[x][cb] *= alpha;
-      }
-      float p[16], sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        p[i] = fast_exp2(fmaf(S[x][i], sc, -m[x]));
-        sum += p[i];
-      }
-      l[x] += sum;
-#pragma unroll
-      for (int y = 0; y < 2; ++y)
-        pf[x][y] = (u32x4){pack_bf16x2(p[8 * y], p[8 * y + 1]), pack_bf16x2(p[8 * y + 2], p[8 * y + 3]),
-                           pack_bf16x2(p[8 * y + 4], p[8 * y + 5]), pack_bf16x2(p[8 * y + 6], p[8 * y + 7])};
-    }
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int y = 0; y < 2; ++y)
-#pragma unroll
-      for (int cb = 0; cb < 4; ++cb) {
-        const u32x4 vf = value_part(vb, u, y, cb);
-#pragma unroll
-        for (int x = 0; x < NB; ++x)
-          O[x][cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf), as_bf16x8(pf[x][y]), O[x][cb], 0, 0, 0);
-      }
-    __builtin_amdgcn_sched_barrier(0);
   };
-  // What lies where no token is may be anything, and 0 x NaN is not 0: such values are cleared in LDS.
-  const auto clear_values = [&](unsigned char* vb, unsigned long long valid) {
-    for (int i = threadIdx.x; i < kStep * (kHeadDim / 8); i += kChunkT) {
+  // exp2 of the logits relative to m, rounded for the second product, and their sum.  The running maximum is not followed
+  // key by key: a sum that stays below 2^16 has lost nothing to being formed relative to an older maximum.  Only where one
+  // does not (the first keys of a row, relative to kNegBig, always), the maximum of these logits is taken, sums so far are
+  // scaled to it where it exceeds the old one by 2^8, and the exponentials are formed again.
+  const auto exponential = [&](float x) { return fast_exp2(fmaf(x, sc, -m)); };
+  const auto follow_maximum = [&](f32x16& S, float& sum, u32x4 (&pf)[2]) {
+    const float mx = top16(S, sc);
+    const bool up = mx > m + kLazy;
+    const float mn = up ? mx : m, alpha = fast_exp2(m - mn);
+    m = mn;
+    l *= alpha;
+#pragma unroll
+    for (int cb = 0; cb < 4; ++cb) O[cb] *= alpha;
+    sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float x = exponential(S[2 * j]), y = exponential(S[2 * j + 1]);
+      sum += x + y;
+      pf[j / 4][j % 4] = pack_bf16x2(x, y);
+    }
+  };
+  // What lies where no token is may be anything, and 0 x NaN is not 0: the wavefront that brought such values clears them
+  // once they are there.
+  const auto clear_values = [&](auto slot, unsigned long long valid) {
+    if (valid == ~0ull) return;
+    unsigned char* vb = s_tiles + (2 + decltype(slot)::value) * kKeyBytes + first_tok * 256;
+    const uint32_t live = (uint32_t)(valid >> (TOK ? first_tok : first_tok / kAttnPage * kAttnPage));
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      u32x4* at = reinterpret_cast<u32x4*>(vb + j * 1024 + lane * 16);
       if (TOK) {
-        if (!((valid >> (i / 16)) & 1ull)) *reinterpret_cast<u32x4*>(vb + i * 16) = (u32x4){0u, 0u, 0u, 0u};
+        if (!((live >> (4 * j + lane / 16)) & 1u)) *at = (u32x4){0u, 0u, 0u, 0u};
       } else {  // eight tokens of a channel
-        const uint32_t bits = (uint32_t)(valid >> (i / 256 * 16 + i % 2 * 8)) & 0xffu;
-        if (bits == 0xffu) continue;
-        u32x4* at = reinterpret_cast<u32x4*>(vb + i * 16);
+        const uint32_t bits = live >> (8 * (lane / 16 % 2));
         u32x4 v = *at;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -346,53 +359,138 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
     }
   };
 
-  look_up(it0);
-  if (it0 < it1) issue(it0);
-  for (int it = it0; it < it1; ++it) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // this wavefront's share of the step has landed
-    __syncthreads();                                             // everyone's has, and the other buffer is free
-    unsigned char* kb = s_tiles + (it & 1) * 2 * kKeyBytes;
-    unsigned char* vb = kb + kKeyBytes;
-    const u32x2 bits = *reinterpret_cast<const u32x2*>(s_valid[it & 1]);
-    const unsigned long long valid = (unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((int)bits.y) << 32 |
-                                     (uint32_t)__builtin_amdgcn_readfirstlane((int)bits.x);
-    if (valid != ~0ull) {
-      clear_values(vb, valid);
-      __syncthreads();
-    }
-    if (it + 1 < it1) issue(it + 1);
-    if (!working || it * kStep > sees_last) continue;
-    const bool masked = valid != ~0ull || it * kStep + kStep - 1 > sees_first;
+  // A value that is not finite belongs to the rows that see its key, and 0 x NaN would carry it to the others of the tile.
+  // Where there are such values among partly seen keys, the unit's keys with any are added one by one, for the rows that
+  // see them, and leave the operand.
+  const auto keep_future_out = [&](int key0, u32x4 (&vf)[2][4], u32x4 (&pf)[2]) {
+    uint32_t odd = 0;  // bit 8 y + e: key 16 y + 8 h + e has one among this lane's channels
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int cb = 0; cb < 4; ++cb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          odd |= (vf[y][cb][i] & 0x7f80u) == 0x7f80u ? 1u << (8 * y + 2 * i) : 0u;
+          odd |= (vf[y][cb][i] & 0x7f800000u) == 0x7f800000u ? 2u << (8 * y + 2 * i) : 0u;
+        }
+    if (!__any(odd != 0u)) return;
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
 #pragma unroll 1
-    for (int u = 0; u < 2; ++u) unit(kb, vb, u, it * kStep + 32 * u, masked, (uint32_t)(valid >> (32 * u)));
+      for (int k = 0; k < 16; ++k) {  // key 16 y + k, element k % 8 of the lanes of half k / 8
+        if (!__any(h == k / 8 && (odd >> (8 * y + k % 8) & 1u))) continue;
+        const uint32_t mine = h == k / 8 ? k & 1 ? 0xffff0000u : 0xffffu : 0u;
+        const u32x4 sel = {k % 8 / 2 == 0 ? mine : 0u, k % 8 / 2 == 1 ? mine : 0u, k % 8 / 2 == 2 ? mine : 0u, k % 8 / 2 == 3 ? mine : 0u};
+        const bool seen = key0 + 16 * y + k <= last;
+#pragma unroll
+        for (int cb = 0; cb < 4; ++cb) {
+          const f32x16 sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[y][cb] & sel), as_bf16x8(pf[y] & sel), O[cb], 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) O[cb][i] = seen ? sum[i] : O[cb][i];
+          vf[y][cb] &= ~sel;
+        }
+      }
+  };
+  const auto partly = [&](int it, unsigned long long valid) { return valid != ~0ull || it * kStep + kStep - 1 > sees_first; };
+  // A unit is 32 keys.  Its exponentials (S holds its logits) stand beside the next unit's products, a matrix instruction
+  // and what fits under it at a time; then its values are added while the keys of the unit after the next come in.  So
+  // in step `it` the values of `it` are read and the keys of it + 1.
+  bf16x8 kf[8];
+  f32x16 S;
+  unsigned long long valid0 = 0, valid1 = 0;  // tokens that exist: of the step, and of the next one
+  const auto fence = []() { __builtin_amdgcn_sched_barrier(0); };
+  const auto step = [&](int it, auto slot) {
+    constexpr std::integral_constant<int, 1 - decltype(slot)::value> other{};
+    __builtin_amdgcn_s_waitcnt(0);  // this wavefront's share has landed
+    clear_values(slot, valid0);
+    __syncthreads();                // everyone's has, and what the last step used is free
+    off_v = off_k;
+    issue_values(other);  // (behind the last step: from the pools' beginning, and unused)
+    const unsigned long long valid2 = issue_keys(it + 2, slot);
+    const bool masked0 = partly(it, valid0), masked1 = it + 1 < it1 && partly(it + 1, valid1);
+    const unsigned long long seen0 = valid0, seen1 = valid1;
+    valid0 = valid1;
+    valid1 = valid2;
+    if (!working) return;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      f32x16 N;
+      const uint32_t keys = use_late(key_at);
+      u32x4 vf[2][4], pf[2];
+      float sums[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        fence();
+        N = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[j], qf[j], j == 0 ? f32x16{} : N, 0, 0, 0);
+        read_value(slot, u, j / 4, j % 4, vf[j / 4][j % 4]);
+        const float x = exponential(S[2 * j]), y = exponential(S[2 * j + 1]);
+        sums[j] = x + y;
+        pf[j / 4][j % 4] = pack_bf16x2(x, y);
+      }
+      fence();
+      float sum = ((sums[0] + sums[1]) + (sums[2] + sums[3])) + ((sums[4] + sums[5]) + (sums[6] + sums[7]));
+      if (__any(!(sum <= kSumLimit))) follow_maximum(S, sum, pf);
+      l += sum;
+      if (masked0) keep_future_out(it * kStep + 32 * u, vf, pf);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        fence();
+        O[j % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(vf[j / 4][j % 4]), as_bf16x8(pf[j / 4]), O[j % 4], 0, 0, 0);
+        read_key(keys, other, u, j, kf[j]);  // (behind the last step: of keys that are not there, and go unused)
+      }
+      fence();
+      S = N;
+      if (u == 0 ? masked0 : masked1) mask(S, it * kStep + 32 * (u + 1), (uint32_t)(u == 0 ? seen0 >> 32 : seen1));
+    }
+  };
+  if (it0 < it1) {
+    look_up(it0);
+    valid0 = issue_keys(it0, std::integral_constant<int, 0>{});
+    off_v = off_k;
+    issue_values(std::integral_constant<int, 0>{});
+    valid1 = issue_keys(it0 + 1, std::integral_constant<int, 1>{});
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (working) {  // the first unit's logits, and the keys of the second
+      constexpr std::integral_constant<int, 0> slot{};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) read_key(key_at, slot, 0, j, kf[j]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[j], qf[j], j == 0 ? f32x16{} : S, 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) read_key(key_at, slot, 1, j, kf[j]);
+      if (partly(it0, valid0)) mask(S, it0 * kStep, (uint32_t)valid0);
+    }
+  }
+  for (int it = it0; it < it1; it += 2) {
+    step(it, std::integral_constant<int, 0>{});
+    if (it + 1 < it1) step(it + 1, std::integral_constant<int, 1>{});
   }
 
+  const SwapPair sw = swap_rows32(__float_as_uint(l));
+  const float sum = __uint_as_float(sw.a) + __uint_as_float(sw.b);
+  if (r >= rows) return;
+  if (pl.parts > 1) {
+    const int64_t at_row = ((int64_t)at * c.n_kv_heads + g) * kRows + r;
+    float* part = a.partial + at_row * kHeadDim;
 #pragma unroll
-  for (int x = 0; x < NB; ++x) {
-    const SwapPair sw = swap_rows32(__float_as_uint(l[x]));
-    const float sum = __uint_as_float(sw.a) + __uint_as_float(sw.b);
-    if (!real[x]) continue;
-    if (pl.parts > 1) {
-      float* o = a.partial + (((int64_t)at * c.n_kv_heads + g) * kRows + (wave * NB + x) * 32 + col) * kRowStride;
+    for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
-      for (int cb = 0; cb < 4; ++cb)
-#pragma unroll
-        for (int i = 0; i < 16; i += 2)
-          *reinterpret_cast<float2*>(o + 32 * cb + 8 * (i / 4) + 4 * h + i % 4) = make_float2(O[x][cb][i], O[x][cb][i + 1]);
-      if (h == 0) *reinterpret_cast<float2*>(o + kHeadDim) = make_float2(m[x], sum);
-    } else {
-      const int64_t row = (lane_row0 + tok[x]) * c.n_q_heads + (int64_t)g * G + head[x];
-      const float inv = sum > 0.f ? 1.f / sum : 0.f;
-      bf16_t* o = a.out + row * kHeadDim;
-#pragma unroll
-      for (int cb = 0; cb < 4; ++cb)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4)
-          *reinterpret_cast<u32x2*>(o + 32 * cb + 2 * i + 4 * h) =
-              (u32x2){pack_bf16x2(O[x][cb][i] * inv, O[x][cb][i + 1] * inv), pack_bf16x2(O[x][cb][i + 2] * inv, O[x][cb][i + 3] * inv)};
-      if (a.out_lse && h == 0) a.out_lse[row] = sum > 0.f ? (m[x] + __log2f(sum)) * kLn2 : -INFINITY;
-    }
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<float4*>(part + 32 * cb + 2 * i + 4 * h) = make_float4(O[cb][i], O[cb][i + 1], O[cb][i + 2], O[cb][i + 3]);
+    if (h == 0) a.part_stats[at_row] = make_float2(m, sum);
+    return;
   }
+  const int64_t row = packed_row((int)use_late((uint32_t)r));
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  bf16_t* o = a.out + row * kHeadDim + 4 * h;
+#pragma unroll
+  for (int cb = 0; cb < 4; ++cb)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+      *reinterpret_cast<u32x2*>(o + 32 * cb + 2 * i) =
+          (u32x2){pack_bf16x2(O[cb][i] * inv, O[cb][i + 1] * inv), pack_bf16x2(O[cb][i + 2] * inv, O[cb][i + 3] * inv)};
+  if (a.out_lse && h == 0) a.out_lse[row] = sum > 0.f ? (m + __log2f(sum)) * kLn2 : -INFINITY;
 }
 
 // The parts of a tile joined: a wavefront per row, a lane per two channels.
@@ -405,21 +503,39 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(CacheView c, ChunkAtte
   const ChunkSeq s = chunk_seq(c, a.ch, pl.b);
   const int G = c.group, t0 = pl.tile * a.tile_tokens, rows = min(a.tile_tokens, s.n - t0) * G;
   const int lane = threadIdx.x % kWave;
+  const int64_t next = (int64_t)c.n_kv_heads * tile_rows;  // rows from part to part
   // the tile's parts share its rows
-  for (int r = pl.part + pl.parts * (threadIdx.x / kWave + 4 * blockIdx.y); r < rows; r += pl.parts * 4 * gridDim.y) {
-    const float* p = a.partial + (((int64_t)pl.first * c.n_kv_heads + g) * tile_rows + r) * kRowStride;
-    const int64_t next = (int64_t)c.n_kv_heads * tile_rows * kRowStride;
+  for (int r = pl.part + pl.parts * (threadIdx.x / kWave); r < rows; r += pl.parts * 4) {
+    const int64_t row0 = ((int64_t)pl.first * c.n_kv_heads + g) * tile_rows + r;
+    const float* p = a.partial + row0 * kHeadDim;
+    const float2* stats = a.part_stats + row0;
     float m = kNegBig;
-    for (int i = 0; i < pl.parts; ++i) m = fmaxf(m, p[i * next + kHeadDim]);
+    for (int i = lane; i < pl.parts; i += kWave) m = fmaxf(m, stats[i * next].x);
+    m = wave_max_f32(m);
     float l = 0.f, x = 0.f, y = 0.f;
-    for (int i = 0; i < pl.parts; ++i) {
-      const float2 ml = *reinterpret_cast<const float2*>(p + i * next + kHeadDim);
-      const float2 o = *reinterpret_cast<const float2*>(p + i * next + 2 * lane);
-      const float w = fast_exp2(ml.x - m);
-      l = fmaf(ml.y, w, l);
-      x = fmaf(o.x, w, x);
-      y = fmaf(o.y, w, y);
+    for (int i0 = 0; i0 < pl.parts; i0 += kWave) {
+      const int n = min(kWave, pl.parts - i0);
+      float w = 0.f;
+      if (lane < n) {
+        const float2 ml = stats[(i0 + lane) * next];
+        w = fast_exp2(ml.x - m);
+        l = fmaf(ml.y, w, l);
+      }
+      const float* o = p + i0 * next * kHeadDim + 2 * lane;
+      for (int i = 0; i < n; i += 4) {  // (absent ones weigh nothing, and read the last)
+        float2 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const float2*>(o + min(i + u, n - 1) * next * kHeadDim);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float wu = i + u < n ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), (i + u) % kWave)) : 0.f;
+          x = fmaf(v[u].x, wu, x);
+          y = fmaf(v[u].y, wu, y);
+        }
+      }
     }
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) l += __shfl_xor(l, d);
     const int t = r / G;
     const int64_t row = (int64_t)(s.row + t0 + t) * c.n_q_heads + (int64_t)g * G + r - t * G;
     const float inv = l > 0.f ? 1.f / l : 0.f;
@@ -430,19 +546,21 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(CacheView c, ChunkAtte
 
 ChunkPlan plan_chunk_attend(const CacheView& c, int n_tokens) {
   ChunkPlan p;
-  // 64 rows to a wavefront read LDS half as often for the same products; 32 where a sequence has few rows on average
-  const int64_t rows = (int64_t)n_tokens * c.group;
-  p.blocks = rows > 128ll * c.batch ? 2 : 1;
-  p.tile_rows = 128 * p.blocks;
+  // 32 bits reach every row of a token-major pool below 4 GiB
+  p.far = c.v_token_major && (c.n_phys_pages * c.stride_page + kMaxGroup * kHeadDim) * (int64_t)sizeof(bf16_t) >= (int64_t)1 << 32;
+  // 256 rows to a workgroup share what it reads; 128 where a sequence has no more on average (not with 64-bit offsets, for
+  // which the registers of that form do not suffice)
+  p.tile_rows = p.far || (int64_t)n_tokens * c.group > 128ll * c.batch ? 256 : 128;
   p.tile_tokens = p.tile_rows / c.group;
-  p.target = 512;
+  p.slots = 256 * (256 / p.tile_rows);
+  const int64_t most = (int64_t)p.slots * kChunkRounds;
   const int64_t at_least = ((int64_t)n_tokens + p.tile_tokens - 1) / p.tile_tokens * c.n_kv_heads;
-  int64_t tiles = ((int64_t)n_tokens / p.tile_tokens + c.batch);
+  int64_t tiles = (int64_t)n_tokens / p.tile_tokens + c.batch;
   if (tiles > n_tokens) tiles = n_tokens;
   tiles *= c.n_kv_heads;
-  p.cuts = at_least < p.target;
-  p.workgroups = p.cuts && tiles < p.target ? p.target : tiles;
-  p.total_bytes = p.cuts ? (size_t)ROCKETKV_WS_HEADER_BYTES + (size_t)p.target * p.tile_rows * kRowStride * sizeof(float) : 0;
+  p.cuts = at_least < most;
+  p.workgroups = p.cuts && tiles < most ? most : tiles;
+  p.total_bytes = p.cuts ? (size_t)ROCKETKV_WS_HEADER_BYTES + (size_t)most * p.tile_rows * (kHeadDim + 2) * sizeof(float) : 0;
   return p;
 }
 
@@ -455,20 +573,19 @@ hipError_t launch_chunk_attend(const CacheView& c, const ChunkView& ch, const bf
   a.out = out;
   a.out_lse = out_lse;
   a.partial = plan.cuts ? reinterpret_cast<float*>(static_cast<char*>(ws) + ROCKETKV_WS_HEADER_BYTES) : nullptr;
+  a.part_stats = reinterpret_cast<float2*>(a.partial + (int64_t)plan.slots * kChunkRounds * plan.tile_rows * kHeadDim);
   a.tile_tokens = plan.tile_tokens;
-  a.target = plan.target;
-  const dim3 grid((unsigned)plan.workgroups), block(kChunkT);
-  const size_t lds = 2 * 2 * kKeyBytes;
-  if (plan.blocks == 1) {
-    if (c.v_token_major) hipLaunchKernelGGL((chunk_attend_kernel<true, 1>), grid, block, lds, st, c, a);
-    else hipLaunchKernelGGL((chunk_attend_kernel<false, 1>), grid, block, lds, st, c, a);
-  } else {
-    if (c.v_token_major) hipLaunchKernelGGL((chunk_attend_kernel<true, 2>), grid, block, lds, st, c, a);
-    else hipLaunchKernelGGL((chunk_attend_kernel<false, 2>), grid, block, lds, st, c, a);
-  }
+  a.slots = plan.slots;
+  const auto launch = [&](auto kernel, int waves) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)plan.workgroups), dim3(waves * kWave), 4 * kKeyBytes, st, c, a);
+  };
+  if (plan.far) launch(chunk_attend_kernel<true, true, 8>, 8);
+  else if (plan.tile_rows == 256 && c.v_token_major) launch(chunk_attend_kernel<true, false, 8>, 8);
+  else if (plan.tile_rows == 256) launch(chunk_attend_kernel<false, false, 8>, 8);
+  else if (c.v_token_major) launch(chunk_attend_kernel<true, false, 4>, 4);
+  else launch(chunk_attend_kernel<false, false, 4>, 4);
   if (plan.cuts) {
-    const unsigned wgs = (unsigned)(plan.workgroups < plan.target ? plan.workgroups : plan.target);
-    hipLaunchKernelGGL(chunk_merge_kernel, dim3(wgs), dim3(256), 0, st, c, a, plan.tile_rows);
+    hipLaunchKernelGGL(chunk_merge_kernel, dim3(plan.slots * kChunkRounds), dim3(256), 0, st, c, a, plan.tile_rows);
   }
   return hipGetLastError();
 }

@@ -400,10 +400,10 @@ hipError_t launch_append_chunk(const CacheView& c, const ChunkView& ch, const Ro
                                const bf16_t* q, int64_t q_stride, bf16_t* q_out, const bf16_t* k, int64_t k_stride,
                                const bf16_t* v, int64_t v_stride, bf16_t* kmax, bf16_t* kmin, void* ws, hipStream_t st);
 struct ChunkPlan {
-  int blocks;       // blocks of 32 rows to a wavefront
   int tile_rows, tile_tokens;
-  int target;       // workgroups wanted where there are fewer tiles
-  bool cuts;        // there may be fewer
+  bool far;         // a token-major pool's rows need 64 bits of offset
+  int slots;        // workgroups the chip holds at a time
+  bool cuts;        // keys may be divided
   int64_t workgroups;
   size_t total_bytes;
 };

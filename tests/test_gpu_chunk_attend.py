@@ -106,6 +106,55 @@ def test_future_keys_that_are_not_finite():
     ref.check_attention(want, out[:seen], lse[:seen])
 
 
+@pytest.mark.parametrize("ps,token_major", [(16, False), (4, True)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("lens,news", [([90], [70]), ([300, 70], [200, 3])])
+def test_future_values_that_are_not_finite(ps, token_major, bad, lens, news):
+    """Rows in front of such a token do not notice it; rows behind it carry what the formula gives."""
+    c = ref.Case(16, lens, news, 4, 2, ps, token_major, shuffled=False)
+    where = {0: [lens[0] - 40, lens[0] - 39, lens[0] - 9], 1: []}
+    if len(lens) > 1:
+        where[1] = [lens[1] - 1]
+    clean, clean_lse = attend(c)
+    want, _, _, _ = ref.attention(c)
+    for b, tokens in where.items():
+        for n, t in enumerate(tokens):
+            at = b * c.cache.pages_cap + t // ps
+            if token_major:
+                c.cache.v_pool[at, :, t % ps, n::7] = bad
+            else:
+                c.cache.v_pool[at, :, n::7, t % ps] = bad
+    out, lse = attend(c)
+    assert torch.equal(lse, clean_lse)
+    for b, n in enumerate(lens):
+        for i in range(news[b]):
+            row = c.starts[b] + i
+            hit = torch.zeros(128, dtype=torch.bool, device="cuda")
+            for k, t in enumerate(where[b]):
+                if t <= n - news[b] + i:
+                    hit[k::7] = True
+            assert (~torch.isfinite(out[row][:, hit])).all()
+            assert torch.equal(out[row][:, ~hit], clean[row][:, ~hit]), f"sequence {b}, row {i}"
+
+
+def test_pool_beyond_32_bits():
+    """Rows of a token-major pool of more than 4 GiB, at its far end too."""
+    c = ref.Case(17, [500, 70], [100, 1], 8, 2, 16, True, shuffled=False)
+    out, lse = attend(c)
+    pages = (5 << 30) // (2 * 16 * 128 * 2)
+    big = rk.alloc_cache(2, 8, 2, 128, 16, c.cache.pages_cap, "cuda", n_phys_pages=pages, v_layout=rk.V_TOKEN_MAJOR)
+    table = torch.randperm(pages, generator=torch.Generator().manual_seed(0))[:2 * big.pages_cap]
+    table[0], table[1], table[40] = pages - 1, 0, pages - 2
+    big.block_table = table.reshape(2, -1).to(torch.int32).cuda()
+    at = table.cuda()
+    big.k_pool[at], big.v_pool[at] = c.cache.k_pool[:len(at)], c.cache.v_pool[:len(at)]
+    big.seq_lens.copy_(c.cache.seq_lens)
+    c.cache = big
+    far, far_lse = attend(c)
+    assert torch.equal(far[c.rows_of(0)], out[c.rows_of(0)])
+    ref.check_attention(c, far, far_lse)
+
+
 def test_more_new_tokens_than_the_cache_holds():
     """Rows in front of the cache's first token see nothing."""
     c = ref.Case(9, [10], [25], 4, 1)
