@@ -9,6 +9,8 @@
 // and a lane owns one key: the 16 rows of a product are added up in its registers, one add a row, with no exchange but
 // the last one with the lane 32 further.  A workgroup owns its keys over all rows, so nothing is added atomically and
 // sums do not depend on the order of workgroups.
+#include <type_traits>
+
 #include "attend_core.h"
 
 namespace rkv {
@@ -17,11 +19,20 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kWeightT = 256;
-constexpr int kRowStep = 64;                                       // query rows per step
+constexpr int kWeightWaves = 4, kKeyWaves = 2;  // half of them hold the same keys
+constexpr int kRowStep = 128;                                           // query rows per step
 constexpr int kRowStepBytes = kRowStep * kHeadDim * (int)sizeof(bf16_t);
 
-__device__ __forceinline__ void to_lds(const bf16_t* src, unsigned char* dst) {
+// 16 bytes per lane, `off` bytes behind a base that is the same for the wavefront, straight to LDS
+__device__ __forceinline__ void to_lds(const void* base, uint32_t off, unsigned char* dst) {
+#ifdef __HIP_DEVICE_COMPILE__
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, -1, 0x00020000),
+                                           (__attribute__((address_space(3))) void*)dst, 16, (int)off, 0, 0, 0);
+#endif
+}
+
+// from any address
+__device__ __forceinline__ void to_lds_far(const void* src, unsigned char* dst) {
 #ifdef __HIP_DEVICE_COMPILE__
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
                                    (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
@@ -38,15 +49,22 @@ struct WeightArgs {
   float* w_out;
 };
 
-// NK: blocks of 32 keys to a wavefront
-template <int NK>
-__global__ __launch_bounds__(kWeightT) __attribute__((amdgpu_waves_per_eu(2)))
+// A wavefront holds 64 keys.  Two take the first 64 rows of a step, two the same keys and the other 64: a workgroup is done
+// with 128 keys in half the time that four wavefronts of keys of their own take for 256, and the last ones of a launch leave
+// less of the chip idle (2048 tokens of 32 heads over 34816 keys and 8 KV heads, us: 673 with 256 keys, two and an eighth
+// rounds of workgroups over the chip; 644 so; eight wavefronts and 256 keys, one workgroup to a compute unit, 705; 32 keys to
+// a wavefront 743).  A unit is 32 rows; its exponentials stand beside the next unit's products, as in the attention, so in
+// step `it` the rows of step it + 1 are read.
+constexpr int NK = 2;  // blocks of 32 keys to a wavefront
+__global__ __launch_bounds__(kWeightWaves * kWave) __attribute__((amdgpu_waves_per_eu(2)))
 void weights_kernel(CacheView c, WeightArgs a) {
-  __shared__ __align__(16) unsigned char s_q[2][kRowStepBytes];
-  __shared__ __align__(16) float s_lse[2][kRowStep];  // in the log2 domain; +inf: a row without any key
-  constexpr int kKeys = 4 * 32 * NK;
+  __shared__ __align__(256) unsigned char s_q[2][kRowStepBytes];  // [128 rows][16 chunks], chunk x of row r at x ^ r % 16
+  __shared__ __align__(16) float s_lse[4][kRowStep];              // in the log2 domain; +inf: a row that adds nothing
+  __shared__ float s_sum[kKeyWaves * 32 * NK];
+  constexpr int kKeys = kKeyWaves * 32 * NK;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int col = lane % 32, h = lane / 32;
+  const int kw = wave % kKeyWaves, own_rows = wave / kKeyWaves * 64;  // which 64 keys, and where in a step its rows begin
   const int unit = blockIdx.y, b = unit / c.n_kv_heads, g = unit % c.n_kv_heads;
   const int G = c.group, ps = c.page_size, cap = c.pages_cap * ps;
   const int n_now = c.seq_lens[b], len = n_now < 0 ? 0 : min(n_now, cap);
@@ -55,15 +73,13 @@ void weights_kernel(CacheView c, WeightArgs a) {
   const int row0 = chunk_first(a.ch, b), n = chunk_rows(a.ch, b);
   const int old = len - n;  // place in the cache of the first new token (the first ones see nothing if it is negative)
 
+  const int mine = key0 + kw * NK * 32 + col;  // this lane's first key, its next one 32 further
   bf16x8 kf[NK][8];
-  int key[NK];
-  bool there[NK];
 #pragma unroll
   for (int x = 0; x < NK; ++x) {
-    key[x] = key0 + (wave * NK + x) * 32 + col;
-    const int64_t pp = key[x] < len ? phys_page(c, b, key[x] / ps) : -1;
-    there[x] = pp >= 0;
-    const bf16_t* k = c.k_pool + (there[x] ? pp * c.stride_page + (int64_t)g * c.stride_head + (int64_t)(key[x] % ps) * kHeadDim : 0) + h * 8;
+    const int key = mine + 32 * x;
+    const int64_t pp = key < len ? phys_page(c, b, key / ps) : -1;
+    const bf16_t* k = c.k_pool + (pp >= 0 ? pp * c.stride_page + (int64_t)g * c.stride_head + (int64_t)(key % ps) * kHeadDim : 0) + h * 8;
 #pragma unroll
     for (int j = 0; j < 8; ++j) kf[x][j] = as_bf16x8(ld_plain<u32x4>(k + j * 16));
   }
@@ -71,80 +87,195 @@ void weights_kernel(CacheView c, WeightArgs a) {
   // rows (token, head) from the first that sees any of the workgroup's keys
   const int rows = n * G;
   const int it0 = max(0, key0 - old) * G / kRowStep, it1 = (rows + kRowStep - 1) / kRowStep;
-  const auto row_at = [&](int r) {  // of a row below `rows`
-    const int t = r / G;
-    return (int64_t)(row0 + t) * c.n_q_heads + (int64_t)g * G + (r - t * G);
-  };
+  const uint32_t per_G = 65536u / (uint32_t)G + 1u;  // x / G == x * per_G >> 16 for x < 1024
   float lse = 0.f;
-  const auto issue = [&](int it) {  // rows 16 wave .. of the step; chunk x of row r at x ^ r % 16
+  // rows 16 wave .. of the step, and what they are normalised by; rows behind the last one repeat it
+  const auto issue = [&](int it, auto to) {
+    const int r0 = it * kRowStep, left = rows - r0;  // of rows in front of the first step's first row: none
+    if (left <= 0) { lse = -INFINITY; return; }
+    const int t0 = r0 / G, skip = r0 - t0 * G;  // the token the step begins in, and how many of its heads it leaves out
+    const int64_t first = (int64_t)(row0 + t0) * c.n_q_heads + (int64_t)g * G;
+    const auto place = [&](int r) {  // of a row of the step, in rows from `first`
+      const uint32_t x = (uint32_t)(skip + r), t = x * per_G >> 16;
+      return t * (uint32_t)c.n_q_heads + (x - t * (uint32_t)G);
+    };
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int rr = 4 * j + lane / 16;
-      const int r = min(it * kRowStep + wave * 16 + rr, rows - 1);
-      to_lds(a.q + row_at(r) * kHeadDim + ((lane % 16) ^ rr) * 8, s_q[it & 1] + (wave * 16 + 4 * j) * 256);
+    for (int j = 0; j < kRowStep / kWeightWaves / 4; ++j) {
+      const int r = wave * (kRowStep / kWeightWaves) + 4 * j + lane / 16;
+      to_lds(a.q + first * kHeadDim, place(min(r, left - 1)) * 256u + ((lane % 16) ^ r % 16) * 16,
+             s_q[decltype(to)::value] + (wave * (kRowStep / kWeightWaves) + 4 * j) * 256);
     }
-    if (wave == 0) {
-      const int r = it * kRowStep + lane;
-      lse = r < rows ? a.lse[row_at(r)] : -INFINITY;
-    }
+    const int r = wave * kWave + lane;
+    lse = r < kRowStep && r < left ? a.lse[first + place(r)] : -INFINITY;
+  };
+  const auto keep_lse = [&](int it) {
+    if (wave < kRowStep / kWave) s_lse[it & 3][wave * kWave + lane] = lse == -INFINITY ? INFINITY : lse * kLog2e;
   };
   const float sc = kLog2e * 0.08838834764831845f;  // log2(e) / sqrt(128)
+  const uint32_t q_at = (uint32_t)((own_rows + col) * 256 + (h ^ (col & 15)) * 16);
+  const auto read_row = [&](uint32_t at, auto slot, int u, int j, bf16x8& qf) {
+    qf = as_bf16x8(*reinterpret_cast<const u32x4*>(&s_q[0][0] + (at ^ (uint32_t)(32 * j)) + (decltype(slot)::value * kRowStepBytes + u * 8192)));
+  };
+  // Of a unit's rows the first ones may not see a key yet: key j is seen from token j - old of the chunk on.
+  const int last_key = key0 + (kw + 1) * NK * 32 - 1;
+  const auto mask = [&](f32x16 (&S)[NK], int r0) {
+    if ((int64_t)(last_key - old) * G <= r0) return;
+#pragma unroll
+    for (int x = 0; x < NK; ++x) {
+      const int first = max(0, mine + 32 * x - old) * G - r0 - 4 * h;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (8 * (i / 4) + i % 4 < first) S[x][i] = -INFINITY;
+    }
+  };
   float sum[NK] = {};
-  if (it0 < it1) issue(it0);
-  for (int it = it0; it < it1; ++it) {
-    if (wave == 0) s_lse[it & 1][lane] = lse == -INFINITY ? INFINITY : lse * kLog2e;
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  bf16x8 qf[8];
+  f32x16 S[NK];
+  const auto fence = []() { __builtin_amdgcn_sched_barrier(0); };
+  const auto step = [&](int it, auto slot) {
+    constexpr std::integral_constant<int, 1 - decltype(slot)::value> other{};
+    __builtin_amdgcn_s_waitcnt(0);
+    keep_lse(it + 1);
     __syncthreads();
-    if (it + 1 < it1) issue(it + 1);
+    issue(it + 2, slot);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int r0 = it * kRowStep + 32 * u;
-      if (r0 >= rows) continue;
-      const unsigned char* qrow = s_q[it & 1] + (32 * u + col) * 256;
-      f32x16 S[NK];
+      f32x16 N[NK];
+      float part[NK];
+      f32x4 row_lse[4];  // of rows 8 i + 4 h ..
+      const uint32_t at = use_late(q_at);
+      const auto read_lse = [&](int i) { row_lse[i] = *reinterpret_cast<const f32x4*>(&s_lse[it & 3][own_rows + 32 * u + 8 * i + 4 * h]); };
+      read_lse(0);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const bf16x8 qf = as_bf16x8(*reinterpret_cast<const u32x4*>(qrow + (((2 * j + h) ^ (col & 15)) * 16)));
+        fence();
+#pragma unroll
+        for (int x = 0; x < NK; ++x)
+          N[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[j], kf[x][j], j == 0 ? f32x16{} : N[x], 0, 0, 0);
+        // (two products later the operand has been read, and its successor comes in)
+        if (j >= 2) read_row(at, other, u, j - 2, qf[j - 2]);
+        if (j % 2 == 0 && j < 6) read_lse(j / 2 + 1);
 #pragma unroll
         for (int x = 0; x < NK; ++x) {
-          const f32x16 zero = {};
-          S[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[x][j], j == 0 ? zero : S[x], 0, 0, 0);
+          const float e0 = fast_exp2(fmaf(S[x][2 * j], sc, -row_lse[j / 2][2 * j % 4]));
+          const float e1 = fast_exp2(fmaf(S[x][2 * j + 1], sc, -row_lse[j / 2][2 * j % 4 + 1]));
+          part[x] = j == 0 ? e0 + e1 : part[x] + (e0 + e1);
         }
       }
-      f32x4 row_lse[4];  // of rows 8 i + 4 h ..
-#pragma unroll
-      for (int i = 0; i < 4; ++i) row_lse[i] = *reinterpret_cast<const f32x4*>(&s_lse[it & 1][32 * u + 8 * i + 4 * h]);
-      // a row sees key j from token j - old of the chunk on
-      const int first_token = r0 / G;
-      const bool all = key0 + (wave + 1) * NK * 32 - 1 <= old + first_token;
+      fence();
+      read_row(at, other, u, 6, qf[6]);
+      read_row(at, other, u, 7, qf[7]);
 #pragma unroll
       for (int x = 0; x < NK; ++x) {
-        const int first_row = max(0, key[x] - old) * G - r0;
-        float part = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float e[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            e[r] = fast_exp2(fmaf(S[x][4 * i + r], sc, -row_lse[i][r]));
-            if (!all && 8 * i + 4 * h + r < first_row) e[r] = 0.f;
-          }
-          part += (e[0] + e[1]) + (e[2] + e[3]);
-        }
-        sum[x] += part;
+        sum[x] += part[x];
+        S[x] = N[x];
       }
+      mask(S, (it + u) * kRowStep + own_rows + 32 * (1 - u));
+    }
+  };
+  if (it0 < it1) {
+    constexpr std::integral_constant<int, 0> first{};
+    constexpr std::integral_constant<int, 1> second{};
+    issue(it0, first);
+    keep_lse(it0);
+    issue(it0 + 1, second);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) read_row(q_at, first, 0, j, qf[j]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int x = 0; x < NK; ++x)
+        S[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[j], kf[x][j], j == 0 ? f32x16{} : S[x], 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) read_row(q_at, first, 1, j, qf[j]);
+    mask(S, it0 * kRowStep + own_rows);
+    for (int it = it0; it < it1; it += 2) {
+      step(it, first);
+      if (it + 1 < it1) step(it + 1, second);
     }
   }
+  // (the lane counted anew: no register holds it through the loop)
+  const int here = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
 #pragma unroll
   for (int x = 0; x < NK; ++x) {
     const SwapPair sw = swap_rows32(__float_as_uint(sum[x]));
-    const float total = __uint_as_float(sw.a) + __uint_as_float(sw.b);
-    if (h == 0 && key[x] < len) {
-      const int64_t at = (int64_t)unit * cap + key[x];
-      const float before = a.w_in && key[x] < old ? a.w_in[at] : 0.f;
-      a.w_out[at] = there[x] ? before + total : before;
-    }
+    sum[x] = __uint_as_float(sw.a) + __uint_as_float(sw.b);
+    if (own_rows != 0 && here < 32) s_sum[(kw * NK + x) * 32 + here] = sum[x];
   }
+  __syncthreads();
+  if (own_rows != 0 || here >= 32) return;
+#pragma unroll
+  for (int x = 0; x < NK; ++x) {
+    const int at_key = (kw * NK + x) * 32 + here, key = key0 + at_key;
+    if (key >= len) continue;
+    const int64_t at = (int64_t)unit * cap + key;
+    const float before = a.w_in && key < old ? a.w_in[at] : 0.f;
+    a.w_out[at] = phys_page(c, b, key / ps) >= 0 ? before + (sum[x] + s_sum[at_key]) : before;
+  }
+}
+
+// For few rows, where reading the keys once is all there is to it: a wavefront for 32 keys, nothing shared, five times the
+// wavefronts.  The keys come through LDS in whole lines (a lane's own pieces of a row are 32 bytes apart from line to line:
+// so 41.7 us for 16 sequences of 4123 tokens).
+constexpr int kFewT = 256;
+__global__ __launch_bounds__(kFewT) __attribute__((amdgpu_waves_per_eu(4)))
+void weights_few_kernel(CacheView c, WeightArgs a) {
+  __shared__ __align__(256) unsigned char s_k[4][32 * kHeadDim * sizeof(bf16_t)];  // chunk x of row r at x ^ r % 16
+  __shared__ __align__(16) float s_lse[4][32];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int col = lane % 32, h = lane / 32;
+  const int unit = blockIdx.y, b = unit / c.n_kv_heads, g = unit % c.n_kv_heads;
+  const int G = c.group, ps = c.page_size, cap = c.pages_cap * ps;
+  const int n_now = c.seq_lens[b], len = n_now < 0 ? 0 : min(n_now, cap);
+  const int key0 = (blockIdx.x * 4 + wave) * 32, key = key0 + col;
+  if (key0 >= len) return;
+  const int64_t pp = key < len ? phys_page(c, b, key / ps) : -1;
+  const int64_t off = pp >= 0 ? pp * c.stride_page + (int64_t)g * c.stride_head + (int64_t)(key % ps) * kHeadDim : 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int r = 4 * j + lane / 16;
+    const int64_t at = (int64_t)((uint64_t)(uint32_t)__shfl((int)(off >> 32), r) << 32 | (uint32_t)__shfl((int)off, r));
+    to_lds_far(c.k_pool + at + ((lane % 16) ^ r % 16) * 8, s_k[wave] + j * 1024);
+  }
+  const int row0 = chunk_first(a.ch, b), n = chunk_rows(a.ch, b), old = len - n, rows = n * G;
+  const float before = a.w_in && key < old && h == 0 ? a.w_in[(int64_t)unit * cap + key] : 0.f;
+  const float sc = kLog2e * 0.08838834764831845f;  // log2(e) / sqrt(128)
+  float sum = 0.f;
+  u32x4 kf[8];
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (brought and read by this wavefront alone)
+#pragma unroll
+  for (int j = 0; j < 8; ++j) kf[j] = *reinterpret_cast<const u32x4*>(s_k[wave] + col * 256 + (((2 * j + h) ^ (col & 15)) * 16));
+  for (int r0 = max(0, key0 - old) * G / 32 * 32; r0 < rows; r0 += 32) {
+    const int r = min(r0 + col, rows - 1), t = r / G;
+    const int64_t row = (int64_t)(row0 + t) * c.n_q_heads + (int64_t)g * G + (r - t * G);
+    u32x4 qf[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) qf[j] = ld_plain<u32x4>(a.q + row * kHeadDim + h * 8 + j * 16);
+    const float l = a.lse[row];
+    if (h == 0) s_lse[wave][col] = l == -INFINITY || r0 + col >= rows ? INFINITY : l * kLog2e;
+    f32x16 S;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qf[j]), as_bf16x8(kf[j]), j == 0 ? f32x16{} : S, 0, 0, 0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (written and read by this wavefront alone)
+    const int first = max(0, key - old) * G - r0 - 4 * h;  // row of the block that sees the key first
+    float part = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const f32x4 rl = *reinterpret_cast<const f32x4*>(&s_lse[wave][2 * i + 4 * h]);
+      float e[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) e[x] = 2 * i + x < first ? 0.f : fast_exp2(fmaf(S[i + x], sc, -rl[x]));
+      part += (e[0] + e[1]) + (e[2] + e[3]);
+    }
+    sum += part;
+    asm volatile("" ::: "memory");
+  }
+  const SwapPair sw = swap_rows32(__float_as_uint(sum));
+  const float total = __uint_as_float(sw.a) + __uint_as_float(sw.b);
+  if (h == 0 && key < len) a.w_out[(int64_t)unit * cap + key] = pp >= 0 ? before + total : before;
 }
 
 hipError_t launch_weights(const CacheView& c, const ChunkView& ch, const bf16_t* q, const float* lse, const float* w_in,
@@ -156,7 +287,9 @@ hipError_t launch_weights(const CacheView& c, const ChunkView& ch, const bf16_t*
   a.w_in = w_in;
   a.w_out = w_out;
   const int units = c.batch * c.n_kv_heads, cap = c.pages_cap * c.page_size;
-  hipLaunchKernelGGL(weights_kernel<2>, dim3((cap + 255) / 256, units), dim3(kWeightT), 0, st, c, a);
+  const auto grid = [&](int keys) { return dim3((unsigned)((cap + keys - 1) / keys), (unsigned)units); };
+  if ((int64_t)ch.n_tokens * c.group <= 32ll * c.batch) hipLaunchKernelGGL(weights_few_kernel, grid(128), dim3(kFewT), 0, st, c, a);
+  else hipLaunchKernelGGL(weights_kernel, grid(kKeyWaves * 32 * NK), dim3(kWeightWaves * kWave), 0, st, c, a);
   return hipGetLastError();
 }
 
