@@ -449,7 +449,7 @@ int32_t rocketkv_accumulate_weights(const rocketkv_cache_t* cache, const rocketk
  * S <= keep_budget; otherwise the last n_recent tokens and, of the others, the keep_budget - n_recent with the largest
  * weight (ties: lower position; NaN counts as larger than every number).  K, V and weights of the kept tokens go to
  * `dst`, in ascending position, and dst->seq_lens[b] = min(S, keep_budget).  src is left as it is.
- * weights: fp32 [batch][n_kv_heads][src->pages_cap * src->page_size].
+ * weights: fp32 [batch][n_kv_heads][src->pages_cap * src->page_size], 16-byte aligned.
  * dst: a cache with pools and lengths of its own, the same head counts, room for keep_budget tokens, any page size and
  *      V layout (channel-major: page_size 16, for src as well).
  * dst_weights: optional fp32 [batch][n_kv_heads][dst->pages_cap * dst->page_size], distinct from weights; the first

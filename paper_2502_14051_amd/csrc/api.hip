@@ -956,6 +956,7 @@ int32_t rocketkv_weight_evict(const rocketkv_cache_t* src, const float* weights,
   if (int r = check_attend_shape(src, who)) return r;
   if (int r = check_attend_shape(dst, who)) return r;
   if (!weights) return fail(ROCKETKV_INVALID_ARG, "%s: weights must not be NULL", who);
+  if ((uintptr_t)weights & 15) return fail(ROCKETKV_INVALID_ARG, "%s: weights must be 16-byte aligned", who);
   if (keep_budget < 1 || n_recent < 0 || n_recent > keep_budget)
     return fail(ROCKETKV_INVALID_ARG, "%s: need 0 <= n_recent (%d) <= keep_budget (%d), keep_budget >= 1", who, n_recent, keep_budget);
   if (src->batch != dst->batch || src->n_q_heads != dst->n_q_heads || src->n_kv_heads != dst->n_kv_heads)

@@ -413,10 +413,10 @@ hipError_t launch_chunk_attend(const CacheView& c, const ChunkView& ch, const bf
 hipError_t launch_weights(const CacheView& c, const ChunkView& ch, const bf16_t* q, const float* lse, const float* w_in,
                           float* w_out, hipStream_t st);
 struct EvictPlan {
-  int slices;     // histograms per row, 0: none are needed
-  int split;      // workgroups per row in the select
-  int slice_len;  // positions of each
-  size_t kept_off, hist_off, total_bytes;
+  int hist_slices;  // histograms per row, 0: rows are short
+  int split;        // workgroups per row in the select
+  int slice_len;    // positions of each
+  size_t kept_off, hist_off, cand_off, n_cand_off, above_off, total_bytes;
 };
 EvictPlan plan_evict(const CacheView& src, int keep);
 hipError_t launch_evict(const CacheView& src, const float* weights, int n_recent, int keep, const CacheView& dst,

@@ -3,13 +3,16 @@
 //          (ties: lower position), ascending;
 // K and V rows and weights of the kept tokens move to another cache.
 //
-//   histogram  (long rows only) the weights of a slice of 16384 positions counted by bins of their ordered bits
-//   select     every workgroup of a row names the bin of the wanted rank, collects the keys in it, ranks them, counts
-//              what its slice is preceded by, and emits its slice in order
+//   histogram  the weights of a slice of 16384 positions counted by bins of their ordered bits
+//   collect    every slice of 4096 names the bin of the wanted rank, adds its keys in that bin to the row's list and notes
+//              how many lie above it
+//   select     every slice ranks the list, counts what it is preceded by, and emits its kept positions in order
 //   move       64 kept tokens a workgroup
 //
-// The move is what the bytes ask for: kept rows read and written.  The select is latency: two passes over a row that is
-// in L2 after the first.
+// Rows of up to 16384 positions need the last two only: a workgroup then holds a whole row in registers and counts and
+// collects for itself.  Long rows did as well, each workgroup passing over the whole row: 27 us for 8 rows of 131072 beside 5
+// for the histograms, bound by the vector instructions of that pass.
+// The move is what the bytes ask for: kept rows read and written.
 #include "select_core.h"
 #include "vote_bins.h"
 
@@ -21,52 +24,136 @@ constexpr int kEvictT = 1024;
 constexpr int kEvictSlice = 4 * kEvictT;   // positions a workgroup emits at a time
 constexpr int kHistSlice = 16 * kEvictT;   // positions counted into one histogram
 constexpr int kEvictCand = 1024;           // keys of the wanted bin that are ranked by counting
+constexpr int kEvictBatch = 8;             // pieces of four weights a thread has in flight
 
 // Ordered bits of a weight: +0 and -0 are equal, NaN (of either sign) is above every number.
 __device__ __forceinline__ uint32_t weight_key(float w) {
   return w != w ? 0xffffffffu : f32_order_key(w + 0.f);
 }
 
+// fn(position, key) for every position of the row in [from, L), by the whole workgroup; `from` and rows begin at multiples
+// of 16 bytes, and rows hold a multiple of four weights
+template <class Fn>
+__device__ __forceinline__ void four_weights(float4 v, int j, int L, const Fn& fn) {
+  const float w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (j + e < L) fn(j + e, weight_key(w[e]));
+}
+template <class Fn>
+__device__ __forceinline__ void each_weight(const float* row, int from, int L, const Fn& fn) {
+  for (int j0 = from + threadIdx.x * 4; j0 < L; j0 += kEvictBatch * kEvictSlice) {
+    float4 v[kEvictBatch];
+#pragma unroll
+    for (int u = 0; u < kEvictBatch; ++u)
+      if (j0 + u * kEvictSlice < L) v[u] = *reinterpret_cast<const float4*>(row + j0 + u * kEvictSlice);
+#pragma unroll
+    for (int u = 0; u < kEvictBatch; ++u) four_weights(v[u], j0 + u * kEvictSlice, L, fn);
+  }
+}
+
 }  // namespace
 
 struct EvictArgs {
-  const float* w;     // [units][cap]
+  const float* w;       // [units][cap]
   int cap, keep, recent;
-  uint16_t* hist;     // [units][slices][kSelBins]; null: rows are counted by the select itself
-  int slices;         // histograms per row
-  int slice_len;      // positions per workgroup of the select
-  int32_t* kept;      // [units][keep]
-  int32_t* kept_user; // optional copy
-  float* w_out;       // optional, rows of dst_cap
+  // long rows only (hist null: short ones)
+  uint16_t* hist;       // [units][hist_slices][kSelBins]
+  int hist_slices;
+  uint2* cand;          // [units][kEvictCand]: key, position
+  uint32_t* n_cand;     // [units]
+  uint32_t* above;      // [units][split]: keys above the bin in a slice
+  int split;            // slices per row, a workgroup each; of kEvictSlice positions where rows are long
+  int slice_len;
+  int32_t* kept;        // [units][keep]
+  int32_t* kept_user;   // optional copy
+  float* w_out;         // optional, rows of dst_cap
   int dst_cap;
   int32_t* n_out;
 };
+
+struct EvictShared {
+  uint32_t hist[kSelBins];
+  uint2 cand[kEvictCand];
+  uint32_t wsum[kEvictT / kWave];
+  uint32_t n_cand, bin, rank, tau, need, gt, eq;
+};
+
+// The bin of rank `k` among the counts in h[], each thread's four the highest first of the ones left to it, and the rank
+// within it: sh.bin, sh.rank.  Ends with a barrier.
+__device__ __forceinline__ void find_rank(const uint32_t (&h)[4], uint32_t k, EvictShared& sh) {
+  uint32_t above = block_excl_scan<kEvictT>(h[0] + h[1] + h[2] + h[3], sh.wsum);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (above < k && k <= above + h[i]) {
+      sh.bin = (uint32_t)(kSelBins - 1 - (int)threadIdx.x * 4 - i);
+      sh.rank = k - above;
+    }
+    above += h[i];
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ void lds_counts(const EvictShared& sh, uint32_t (&h)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = sh.hist[kSelBins - 1 - threadIdx.x * 4 - i];
+}
+__device__ __forceinline__ void row_counts(const EvictArgs& a, int unit, int L, uint32_t (&h)[4]) {
+  const int n = (L + kHistSlice - 1) / kHistSlice;
+#pragma unroll 4
+  for (int s = 0; s < n; ++s) {
+    const uint2 w = reinterpret_cast<const uint2*>(a.hist + ((int64_t)unit * a.hist_slices + s) * kSelBins)[kEvictT - 1 - threadIdx.x];
+    h[0] += w.y >> 16;
+    h[1] += w.y & 0xffffu;
+    h[2] += w.x >> 16;
+    h[3] += w.x & 0xffffu;
+  }
+}
 
 __global__ __launch_bounds__(kEvictT) void evict_hist_kernel(CacheView c, EvictArgs a) {
   __shared__ uint32_t s_hist[kSelBins];
   const int unit = blockIdx.y, S = c.seq_lens[unit / c.n_kv_heads], L = S - a.recent;
   const int j0 = blockIdx.x * kHistSlice;
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.n_cand[unit] = 0;
   if (S <= a.keep || S > a.cap || j0 >= L) return;
   for (int i = threadIdx.x; i < kSelBins; i += kEvictT) s_hist[i] = 0;
   __syncthreads();
-  const float* row = a.w + (int64_t)unit * a.cap;
-#pragma unroll
-  for (int u = 0; u < kHistSlice / kEvictT; ++u) {
-    const int j = j0 + u * kEvictT + threadIdx.x;
-    if (j < L) atomicAdd(&s_hist[vote_bin(weight_key(row[j]))], 1u);
-  }
+  each_weight(a.w + (int64_t)unit * a.cap, j0, min(L, j0 + kHistSlice), [&](int, uint32_t key) { atomicAdd(&s_hist[vote_bin(key)], 1u); });
   __syncthreads();
-  uint32_t* out = reinterpret_cast<uint32_t*>(a.hist + ((int64_t)unit * a.slices + blockIdx.x) * kSelBins);
+  uint32_t* out = reinterpret_cast<uint32_t*>(a.hist + ((int64_t)unit * a.hist_slices + blockIdx.x) * kSelBins);
   for (int i = threadIdx.x; i < kSelBins / 2; i += kEvictT) out[i] = s_hist[2 * i] | s_hist[2 * i + 1] << 16;
 }
 
-struct EvictShared {
-  uint32_t hist[kSelBins];
-  uint32_t cand[kEvictCand];
-  uint32_t wsum[kEvictT / kWave];
-  uint32_t n_cand, bin, rank, tau, need, gt, eq;
-};
+__global__ __launch_bounds__(kEvictT) void evict_collect_kernel(CacheView c, EvictArgs a) {
+  __shared__ EvictShared sh;
+  const int tid = threadIdx.x, unit = blockIdx.y, S = c.seq_lens[unit / c.n_kv_heads], L = S - a.recent;
+  const int j = blockIdx.x * kEvictSlice + tid * 4;
+  if (S <= a.keep || S > a.cap || (int)blockIdx.x * kEvictSlice >= L || a.keep == a.recent) return;
+  const float* row = a.w + (int64_t)unit * a.cap;
+  const float4 v = j < L ? *reinterpret_cast<const float4*>(row + j) : make_float4(0.f, 0.f, 0.f, 0.f);
+  uint32_t h[4] = {};
+  row_counts(a, unit, L, h);
+  find_rank(h, (uint32_t)(a.keep - a.recent), sh);
+  const KeyRange in = bin_range(sh.bin);
+  uint32_t above = 0;
+  four_weights(v, j, L, [&](int at, uint32_t key) {
+    if (key < in.lo) return;
+    if (key - in.lo > in.span) {
+      ++above;
+    } else {
+      const uint32_t n = atomicAdd(&a.n_cand[unit], 1u);
+      if (n < (uint32_t)kEvictCand) a.cand[(int64_t)unit * kEvictCand + n] = make_uint2(key, (uint32_t)at);
+    }
+  });
+  above = wave_incl_scan(above);
+  if (tid == 0) sh.gt = 0;
+  __syncthreads();
+  if (tid % kWave == kWave - 1) atomicAdd(&sh.gt, above);
+  __syncthreads();
+  if (tid == 0) a.above[(int64_t)unit * a.split + blockIdx.x] = sh.gt;
+}
 
+// SHORT: rows of at most kHistSlice positions, held in registers
+template <bool SHORT>
 __global__ __launch_bounds__(kEvictT) void evict_select_kernel(CacheView c, EvictArgs a) {
   __shared__ EvictShared sh;
   const int tid = threadIdx.x, unit = blockIdx.y, b = unit / c.n_kv_heads, g = unit % c.n_kv_heads;
@@ -95,104 +182,103 @@ __global__ __launch_bounds__(kEvictT) void evict_select_kernel(CacheView c, Evic
   }
   if (j_begin >= L || want == 0) return;
   const float* row = a.w + (int64_t)unit * a.cap;
-  const auto key_at = [&](int j) { return weight_key(row[j]); };
-
-  // bins of the whole row, the highest four of the ones left to each thread
-  uint32_t h[4] = {};
-  if (a.hist) {
-    const int n = (L + kHistSlice - 1) / kHistSlice;
-    for (int s = 0; s < n; ++s) {
-      const uint2 w = reinterpret_cast<const uint2*>(a.hist + ((int64_t)unit * a.slices + s) * kSelBins)[kEvictT - 1 - tid];
-      h[0] += w.y >> 16;
-      h[1] += w.y & 0xffffu;
-      h[2] += w.x >> 16;
-      h[3] += w.x & 0xffffu;
+  constexpr int kHeld = SHORT ? kHistSlice / kEvictSlice : 1;
+  float4 held[kHeld];  // the whole row, or the slice's first weights
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) {
+    const int j = (SHORT ? u * kEvictSlice : j_begin) + tid * 4;
+    held[u] = j < L ? *reinterpret_cast<const float4*>(row + j) : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  const auto each = [&](int upto, const auto& fn) {
+    if (SHORT) {
+#pragma unroll
+      for (int u = 0; u < kHeld; ++u) four_weights(held[u], u * kEvictSlice + tid * 4, upto, fn);
+    } else {
+      each_weight(row, 0, upto, fn);
     }
-  } else {
+  };
+
+  uint32_t h[4] = {};
+  if (tid == 0) sh.n_cand = sh.gt = sh.eq = 0;
+  if (SHORT) {
     for (int i = tid; i < kSelBins; i += kEvictT) sh.hist[i] = 0;
     __syncthreads();
-    for (int j = tid; j < L; j += kEvictT) atomicAdd(&sh.hist[vote_bin(key_at(j))], 1u);
+    each(L, [&](int, uint32_t key) { atomicAdd(&sh.hist[vote_bin(key)], 1u); });
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = sh.hist[kSelBins - 1 - tid * 4 - i];
+    lds_counts(sh, h);
+  } else {
+    row_counts(a, unit, L, h);
   }
-  if (tid == 0) sh.n_cand = sh.gt = sh.eq = 0;
-  // the bin of rank `k` among the counts in h[], and the rank within it; ends with a barrier
-  const auto find = [&](uint32_t k) {
-    uint32_t above = block_excl_scan<kEvictT>(h[0] + h[1] + h[2] + h[3], sh.wsum);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (above < k && k <= above + h[i]) {
-        sh.bin = (uint32_t)(kSelBins - 1 - tid * 4 - i);
-        sh.rank = k - above;
-      }
-      above += h[i];
-    }
-    __syncthreads();
-  };
-  find(want);
+  find_rank(h, want, sh);
   uint32_t k = sh.rank;
   KeyRange in = bin_range(sh.bin);
-  // the keys of the bin; above it, what lies before the slice
+  // the keys of the bin; above it, how many lie before the slice
   uint32_t gt = 0, eq = 0;
-  const auto collect = [&](bool count) {
-    for (int j = tid; j < L; j += kEvictT) {
-      const uint32_t key = key_at(j);
-      if (key < in.lo) continue;
+  const auto collect = [&]() {
+    gt = 0;
+    each(L, [&](int j, uint32_t key) {
+      if (key < in.lo) return;
       if (key - in.lo > in.span) {
-        if (count && j < j_begin) ++gt;
+        gt += j < j_begin ? 1u : 0u;
       } else {
         const uint32_t at = atomicAdd(&sh.n_cand, 1u);
-        if (at < (uint32_t)kEvictCand) sh.cand[at] = key;
+        if (at < (uint32_t)kEvictCand) sh.cand[at] = make_uint2(key, (uint32_t)j);
       }
-    }
+    });
     __syncthreads();
     return (int)sh.n_cand;
   };
-  int n_cand = collect(false);
+  int n_cand;
+  if (SHORT) {
+    n_cand = collect();
+  } else {
+    n_cand = (int)a.n_cand[unit];
+    if (tid < min(n_cand, kEvictCand)) sh.cand[tid] = a.cand[(int64_t)unit * kEvictCand + tid];
+    for (int i = tid; i < (int)blockIdx.x; i += kEvictT) gt += a.above[(int64_t)unit * a.split + i];
+    __syncthreads();
+  }
   while (n_cand > kEvictCand && in.span != 0u) {  // too many to rank: the bin is divided again
     const int shift = part_shift(in);
     __syncthreads();
     for (int i = tid; i < kSelBins; i += kEvictT) sh.hist[i] = 0;
     if (tid == 0) sh.n_cand = 0;
     __syncthreads();
-    for (int j = tid; j < L; j += kEvictT) {
-      const uint32_t key = key_at(j);
+    each(L, [&](int, uint32_t key) {
       if (key >= in.lo && key - in.lo <= in.span) atomicAdd(&sh.hist[(key - in.lo) >> shift], 1u);
-    }
+    });
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = sh.hist[kSelBins - 1 - tid * 4 - i];
-    find(k);
+    lds_counts(sh, h);
+    find_rank(h, k, sh);
     k = sh.rank;
     in = part_range(in, sh.bin, shift);
-    n_cand = collect(false);
+    n_cand = collect();
   }
   uint32_t tau, need;  // the threshold, and how many keys at it are kept
   if (n_cand <= kEvictCand) {
+    const uint2 own = tid < n_cand ? sh.cand[tid] : make_uint2(0u, 0xffffffffu);
     if (tid < n_cand) {
-      const uint32_t mine = sh.cand[tid];
       uint32_t above = 0, upto = 0;
       for (int j = 0; j < n_cand; ++j) {
-        above += sh.cand[j] > mine ? 1u : 0u;
-        upto += sh.cand[j] >= mine ? 1u : 0u;
+        const uint32_t other = sh.cand[j].x;
+        above += other > own.x ? 1u : 0u;
+        upto += other >= own.x ? 1u : 0u;
       }
       if (above < k && k <= upto) {  // equal keys write the same pair
-        sh.tau = mine;
+        sh.tau = own.x;
         sh.need = k - above;
       }
     }
     __syncthreads();
     tau = sh.tau;
     need = sh.need;
+    if (own.y < (uint32_t)j_begin) {
+      gt += own.x > tau ? 1u : 0u;
+      eq += own.x == tau ? 1u : 0u;
+    }
   } else {  // one key left
     tau = in.lo;
     need = k;
-  }
-  for (int j = tid; j < j_begin; j += kEvictT) {
-    const uint32_t key = key_at(j);
-    gt += key > tau ? 1u : 0u;
-    eq += key == tau ? 1u : 0u;
+    each(j_begin, [&](int, uint32_t key) { eq += key == tau ? 1u : 0u; });
   }
   gt = wave_incl_scan(gt);
   eq = wave_incl_scan(eq);
@@ -208,10 +294,19 @@ __global__ __launch_bounds__(kEvictT) void evict_select_kernel(CacheView c, Evic
   // ordered emission: kEvictSlice positions at a time, four neighbours a thread
   for (int j0 = j_begin; j0 < j_end; j0 += kEvictSlice) {
     const int j = j0 + tid * 4;
+    float4 v = held[0];
+    if (SHORT) {
+#pragma unroll
+      for (int u = 1; u < kHeld; ++u)
+        if (j0 == u * kEvictSlice) v = held[u];
+    } else if (j0 != j_begin && j < j_end) {
+      v = *reinterpret_cast<const float4*>(row + j);
+    }
+    const float w[4] = {v.x, v.y, v.z, v.w};
     uint32_t key[4], cnt = 0;  // low 16 bits: keys above the threshold, high 16 bits: keys at it
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      key[e] = j + e < j_end ? key_at(j + e) : 0u;
+      key[e] = weight_key(w[e]);
       if (j + e < j_end) cnt += (key[e] > tau ? 1u : 0u) + (key[e] == tau ? 0x10000u : 0u);
     }
     const uint32_t before = block_excl_scan<kEvictT>(cnt, sh.wsum);
@@ -351,18 +446,24 @@ EvictPlan plan_evict(const CacheView& src, int keep) {
   const size_t units = (size_t)src.batch * src.n_kv_heads;
   const int64_t cap = (int64_t)src.pages_cap * src.page_size;
   const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-  // up to a histogram's length a row is counted by every one of its workgroups for itself
-  p.slices = cap > kHistSlice ? (int)((cap + kHistSlice - 1) / kHistSlice) : 0;
-  int split = (int)((cap + kEvictSlice - 1) / kEvictSlice);
+  const bool is_long = cap > kHistSlice;
+  p.hist_slices = is_long ? (int)((cap + kHistSlice - 1) / kHistSlice) : 0;
+  // a workgroup per slice of 4096 positions; for short rows no more workgroups than one round over the chip
+  p.split = (int)((cap + kEvictSlice - 1) / kEvictSlice);
   const int most = units >= 256 ? 1 : (int)(256 / units);
-  if (split > most) split = most;
-  p.slice_len = (int)(((cap + split - 1) / split + kEvictSlice - 1) / kEvictSlice * kEvictSlice);
-  p.split = (int)((cap + p.slice_len - 1) / p.slice_len);
+  if (!is_long && p.split > most) p.split = most;
+  p.slice_len = (int)(((cap + p.split - 1) / p.split + kEvictSlice - 1) / kEvictSlice * kEvictSlice);
   size_t off = ROCKETKV_WS_HEADER_BYTES;
-  p.kept_off = off;
-  off += up(units * (size_t)keep * sizeof(int32_t));
-  p.hist_off = off;
-  off += up(units * (size_t)p.slices * kSelBins * sizeof(uint16_t));
+  const auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += up(bytes);
+    return at;
+  };
+  p.kept_off = take(units * (size_t)keep * sizeof(int32_t));
+  p.hist_off = take(units * (size_t)p.hist_slices * kSelBins * sizeof(uint16_t));
+  p.cand_off = take(is_long ? units * kEvictCand * sizeof(uint2) : 0);
+  p.n_cand_off = take(is_long ? units * sizeof(uint32_t) : 0);
+  p.above_off = take(is_long ? units * (size_t)p.split * sizeof(uint32_t) : 0);
   p.total_bytes = off;
   return p;
 }
@@ -375,18 +476,28 @@ hipError_t launch_evict(const CacheView& src, const float* weights, int n_recent
   a.cap = src.pages_cap * src.page_size;
   a.keep = keep;
   a.recent = n_recent;
-  a.slices = plan.slices;
-  a.hist = plan.slices ? reinterpret_cast<uint16_t*>(base + plan.hist_off) : nullptr;
+  a.hist_slices = plan.hist_slices;
+  a.hist = plan.hist_slices ? reinterpret_cast<uint16_t*>(base + plan.hist_off) : nullptr;
+  a.cand = reinterpret_cast<uint2*>(base + plan.cand_off);
+  a.n_cand = reinterpret_cast<uint32_t*>(base + plan.n_cand_off);
+  a.above = reinterpret_cast<uint32_t*>(base + plan.above_off);
+  a.split = plan.split;
   a.slice_len = plan.slice_len;
   a.kept = reinterpret_cast<int32_t*>(base + plan.kept_off);
   a.kept_user = kept_idx;
   a.w_out = dst_weights;
   a.dst_cap = dst.pages_cap * dst.page_size;
   a.n_out = dst.seq_lens;
-  const int units = src.batch * src.n_kv_heads;
-  if (plan.slices) hipLaunchKernelGGL(evict_hist_kernel, dim3(plan.slices, units), dim3(kEvictT), 0, st, src, a);
-  hipLaunchKernelGGL(evict_select_kernel, dim3(plan.split, units), dim3(kEvictT), 0, st, src, a);
-  const dim3 grid((keep + 63) / 64, units), block(256);
+  const unsigned units = (unsigned)(src.batch * src.n_kv_heads);
+  const dim3 slices((unsigned)plan.split, units);
+  if (a.hist) {
+    hipLaunchKernelGGL(evict_hist_kernel, dim3((unsigned)plan.hist_slices, units), dim3(kEvictT), 0, st, src, a);
+    hipLaunchKernelGGL(evict_collect_kernel, slices, dim3(kEvictT), 0, st, src, a);
+    hipLaunchKernelGGL(evict_select_kernel<false>, slices, dim3(kEvictT), 0, st, src, a);
+  } else {
+    hipLaunchKernelGGL(evict_select_kernel<true>, slices, dim3(kEvictT), 0, st, src, a);
+  }
+  const dim3 grid((unsigned)((keep + 63) / 64), units), block(256);
   if (src.v_token_major) {
     if (dst.v_token_major) hipLaunchKernelGGL((evict_move_kernel<true, true>), grid, block, 0, st, src, dst, a);
     else hipLaunchKernelGGL((evict_move_kernel<true, false>), grid, block, 0, st, src, dst, a);
