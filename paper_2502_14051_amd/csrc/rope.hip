@@ -41,6 +41,15 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((pair_f32){lo, hi}, pair_bf16));
 }
 
+// STREAM: past the caches.  138 -> 132 us for 32768 tokens of 40 heads; queries on the way into the cache, which is what
+// reads them next, lose by it (712 -> 720 us for 131072 tokens).
+template <bool STREAM>
+__device__ __forceinline__ void st16(bf16_t* p, uint4 v) {
+  const rope_u32x4 x = {v.x, v.y, v.z, v.w};
+  if (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<rope_u32x4*>(p));
+  else *reinterpret_cast<rope_u32x4*>(p) = x;
+}
+
 // s * (cos, sin) of the angles of tokens [0, n) at `pos_of(token)`, all threads of the workgroup
 template <class Pos>
 __device__ __forceinline__ void fill_turns(const RopeView& r, int n, const Pos& pos_of, float2* s_cs) {
@@ -59,15 +68,17 @@ __device__ __forceinline__ void fill_turns(const RopeView& r, int n, const Pos& 
 struct RowPart {
   uint4 own, far;
 };
+// ODD: half a rotation is no multiple of eight channels, and the partners are not eight neighbours at one.
+template <bool ODD>
 __device__ __forceinline__ RowPart request_row(const RopeView& r, const bf16_t* row, int c0) {
   RowPart p;
   p.own = ld16<false>(row + c0);
   p.far = make_uint4(0, 0, 0, 0);
   const int half = r.rot_dim / 2;
   if (!r.interleaved && c0 < r.rot_dim) {
-    if (half % 8 == 0) {
+    if (!ODD) {
       p.far = ld16<false>(row + (c0 < half ? c0 + half : c0 - half));
-    } else {  // the partners are not eight neighbours at a multiple of eight
+    } else {
       uint32_t w[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -79,6 +90,7 @@ __device__ __forceinline__ RowPart request_row(const RopeView& r, const bf16_t* 
   }
   return p;
 }
+inline bool rope_is_odd(const RopeView& r) { return !r.interleaved && r.rot_dim % 16 != 0; }
 // rounded to bf16 once, at the end
 __device__ __forceinline__ uint4 turn_row(const RopeView& r, const RowPart& p, const float2* cs, int c0) {
   const Eight a = unpack8(p.own);
@@ -108,6 +120,7 @@ __device__ __forceinline__ uint4 turn_row(const RopeView& r, const RowPart& p, c
 // `n` tokens of `heads` heads each, from x (rows of x_stride elements a token) to y, by the whole workgroup; the
 // tokens' turns are in s_cs.  Every lane has read all it needs of a row before the wavefront stores into it, and a row
 // belongs to one wavefront, so x and y may be the same memory.
+template <bool STREAM, bool ODD>
 __device__ __forceinline__ void turn_heads(const RopeView& r, const bf16_t* x, int64_t x_stride, bf16_t* y, int64_t y_stride,
                                            int n, int heads, const float2* s_cs) {
   const int c0 = threadIdx.x % kRowLanes * 8, half = r.rot_dim / 2;
@@ -117,19 +130,20 @@ __device__ __forceinline__ void turn_heads(const RopeView& r, const bf16_t* x, i
 #pragma unroll
     for (int u = 0; u < kRowsInFlight; ++u) {
       const int i = i0 + u * kRowsPerPass, t = i / heads, h = i - t * heads;
-      if (i < rows) p[u] = request_row(r, x + t * x_stride + h * kHeadDim, c0);
+      if (i < rows) p[u] = request_row<ODD>(r, x + t * x_stride + h * kHeadDim, c0);
     }
 #pragma unroll
     for (int u = 0; u < kRowsInFlight; ++u) {
       const int i = i0 + u * kRowsPerPass, t = i / heads, h = i - t * heads;
       if (i < rows) {
         const uint4 o = turn_row(r, p[u], s_cs + t * half, c0);
-        *reinterpret_cast<uint4*>(y + t * y_stride + h * kHeadDim + c0) = o;
+        st16<STREAM>(y + t * y_stride + h * kHeadDim + c0, o);
       }
     }
   }
 }
 
+template <bool ODD>
 __global__ __launch_bounds__(kRopeT) void rope_kernel(RopeView r, const int32_t* __restrict__ positions, int n_tokens,
                                                      int heads, const bf16_t* x, int64_t x_stride, bf16_t* y,
                                                      int64_t y_stride, int per_wg) {
@@ -137,7 +151,7 @@ __global__ __launch_bounds__(kRopeT) void rope_kernel(RopeView r, const int32_t*
   const int t0 = blockIdx.x * per_wg, n = min(per_wg, n_tokens - t0);
   fill_turns(r, n, [&](int t) { return positions[t0 + t]; }, s_cs);
   __syncthreads();
-  turn_heads(r, x + t0 * x_stride, x_stride, y + t0 * y_stride, y_stride, n, heads, s_cs);
+  turn_heads<true, ODD>(r, x + t0 * x_stride, x_stride, y + t0 * y_stride, y_stride, n, heads, s_cs);
 }
 
 // What a chunk brings to sequence b.
@@ -157,9 +171,9 @@ __device__ __forceinline__ NewTokens new_tokens(const CacheView& c, const ChunkV
 
 }  // namespace
 
-// New tokens into the cache, in one launch: workgroups [0, kv_wgs) x head groups take blocks of `pages` pages (aligned to
-// `pages`, a multiple of eight, so that a channel's summaries leave as whole 16-byte pieces), the others blocks of query
-// rows.  A block is worked through kBlockTokens tokens at a time: sines of the tokens, then head by head the key rows
+// New tokens into the cache, in one launch: the first workgroups take blocks of `pages` pages (aligned to `pages`, a multiple
+// of eight, so that a channel's summaries leave as whole 16-byte pieces) of some heads, the others blocks of query rows (with
+// the two kinds mixed instead, 131072 tokens took 711 us, so 668).  A block is worked through kBlockTokens tokens at a time: sines of the tokens, then head by head the key rows
 // (turned) and the value rows to the pools and to LDS, from where a thread takes a pair of channels down the tokens of a
 // page: extremes of the keys, in the order of the tokens as single appends would fold them, and the 16 values of a
 // channel-major tile's row.
@@ -174,7 +188,9 @@ struct AppendChunkArgs {
   uint32_t* arrived;  // per sequence at read_slot(): workgroups that have read its length
 };
 
-__global__ __launch_bounds__(kRopeT) void append_chunk_kernel(CacheView c, AppendChunkArgs a) {
+template <bool ODD>
+__global__ __launch_bounds__(kRopeT) __attribute__((amdgpu_waves_per_eu(ODD ? 3 : 4)))
+void append_chunk_kernel(CacheView c, AppendChunkArgs a) {
   extern __shared__ __align__(16) unsigned char s_mem[];
   float2* s_cs = reinterpret_cast<float2*>(s_mem);                                                    // [tokens][pairs]
   uint32_t* s_k = reinterpret_cast<uint32_t*>(s_mem + (size_t)kBlockTokens * kHeadDim / 2 * sizeof(float2));  // [tokens][64]
@@ -187,13 +203,13 @@ __global__ __launch_bounds__(kRopeT) void append_chunk_kernel(CacheView c, Appen
   // anew at any time.
   const auto kv_tiles = [&](int n) { return n > 0 ? (n + span - 2) / span + 1 : 0; };
   const auto q_tiles = [&](int n) { return a.q ? (n + a.q_block - 1) / a.q_block : 0; };
-  const bool is_kv = (int)blockIdx.x < a.kv_wgs * a.head_groups;
+  const int n_kv = a.kv_wgs * a.head_groups;
+  const bool is_kv = (int)blockIdx.x < n_kv;
   int b, tile;
   if (is_kv) {
     if (!locate_tile(c.batch, blockIdx.x / a.head_groups, [&](int i) { return kv_tiles(chunk_rows(a.ch, i)); }, b, tile)) return;
   } else {
-    if (!locate_tile(c.batch, blockIdx.x - a.kv_wgs * a.head_groups, [&](int i) { return q_tiles(chunk_rows(a.ch, i)); }, b, tile))
-      return;
+    if (!locate_tile(c.batch, blockIdx.x - n_kv, [&](int i) { return q_tiles(chunk_rows(a.ch, i)); }, b, tile)) return;
   }
   const NewTokens s = new_tokens(c, a.ch, b);
 
@@ -205,15 +221,16 @@ __global__ __launch_bounds__(kRopeT) void append_chunk_kernel(CacheView c, Appen
       fill_turns(a.rope, n, [&](int t) { return a.positions ? a.positions[r0 + t] : s.old + t0 + t; }, s_cs);
       __syncthreads();
     }
-    turn_heads(a.rope, x, a.q_stride, y, (int64_t)c.n_q_heads * kHeadDim, n, c.n_q_heads, s_cs);
+    turn_heads<false, ODD>(a.rope, x, a.q_stride, y, (int64_t)c.n_q_heads * kHeadDim, n, c.n_q_heads, s_cs);
   } else if (s.room) {
     const int g0 = (int)(blockIdx.x % a.head_groups) * a.heads_per_wg, ng = min(a.heads_per_wg, c.n_kv_heads - g0);
     const int p0 = (s.old / span + tile) * a.pages;
     const int lo = max(s.old, p0 * ps), hi = min(s.old + s.n, p0 * ps + span);  // the block's new tokens
-    const int half = a.rope.rot_dim / 2, c0 = tid % kRowLanes * 8;
-    for (int tb = p0 * ps; tb < hi; tb += kBlockTokens) {
+    const int half = a.rope.rot_dim / 2, c0 = tid % kRowLanes * 8, i0 = tid / kRowLanes;
+    constexpr int kPasses = kBlockTokens / kRowsPerPass;
+    const int first_tb = lo < hi ? p0 * ps + (lo - p0 * ps) / kBlockTokens * kBlockTokens : hi;
+    for (int tb = first_tb; tb < hi; tb += kBlockTokens) {
       const int tl = max(lo, tb), th = min(hi, tb + kBlockTokens);
-      if (tl >= th) continue;
       if (turns) {
         __syncthreads();  // the last block's turns have been used
         fill_turns(a.rope, th - tl, [&](int t) { const int r = s.row + tl + t - s.old; return a.positions ? a.positions[r] : tl + t; }, s_cs);
@@ -221,21 +238,20 @@ __global__ __launch_bounds__(kRopeT) void append_chunk_kernel(CacheView c, Appen
       for (int gi = 0; gi < ng; ++gi) {
         const int g = g0 + gi;
         __syncthreads();  // the turns are there; the last head's rows have been used
-        constexpr int kPasses = kBlockTokens / kRowsPerPass;
         RowPart kp[kPasses];
         uint4 vp[kPasses];
 #pragma unroll
         for (int u = 0; u < kPasses; ++u) {
-          const int t = tl + tid / kRowLanes + u * kRowsPerPass;
+          const int t = tl + i0 + u * kRowsPerPass;
           if (t < th) {
             const int64_t r = s.row + t - s.old;
-            kp[u] = request_row(a.rope, a.k + r * a.k_stride + g * kHeadDim, c0);
+            kp[u] = request_row<ODD>(a.rope, a.k + r * a.k_stride + g * kHeadDim, c0);
             vp[u] = ld16<true>(a.v + r * a.v_stride + g * kHeadDim + c0);
           }
         }
 #pragma unroll
         for (int u = 0; u < kPasses; ++u) {
-          const int i = tid / kRowLanes + u * kRowsPerPass, t = tl + i;
+          const int i = i0 + u * kRowsPerPass, t = tl + i;
           if (t < th) {
             const uint4 k = turns ? turn_row(a.rope, kp[u], s_cs + i * half, c0) : kp[u].own;
             *reinterpret_cast<uint4*>(s_k + i * (kHeadDim / 2) + c0 / 2) = k;
@@ -352,8 +368,8 @@ hipError_t launch_rope(const RopeView& r, const int32_t* positions, int n_tokens
   int per_wg = (n_tokens + 2047) / 2048;
   if (per_wg > kBlockTokens) per_wg = kBlockTokens;
   const size_t lds = (size_t)per_wg * (r.rot_dim / 2) * sizeof(float2);
-  hipLaunchKernelGGL(rope_kernel, dim3((n_tokens + per_wg - 1) / per_wg), dim3(kRopeT), lds, st, r, positions, n_tokens,
-                     n_heads, x, x_stride, y, y_stride, per_wg);
+  hipLaunchKernelGGL(rope_is_odd(r) ? rope_kernel<true> : rope_kernel<false>, dim3((n_tokens + per_wg - 1) / per_wg),
+                     dim3(kRopeT), lds, st, r, positions, n_tokens, n_heads, x, x_stride, y, y_stride, per_wg);
   return hipGetLastError();
 }
 
@@ -374,13 +390,16 @@ hipError_t launch_append_chunk(const CacheView& c, const ChunkView& ch, const Ro
   a.q_out = q_out;
   a.kmax = kmax;
   a.kmin = kmin;
+  // Blocks of about 128 tokens; smaller ones where there are few.
   int pages = ((128 + c.page_size - 1) / c.page_size + 7) / 8 * 8;
   if (pages > 32) pages = 32;  // 16 KiB of summaries a head
+  const auto blocks = [&](int pages) {  // n tokens touch at most n / span + 2, and no more than there are tokens
+    const int64_t x = (int64_t)ch.n_tokens / (pages * c.page_size) + 2ll * c.batch;
+    return (int)(x < ch.n_tokens ? x : ch.n_tokens);
+  };
+  while (pages > 8 && (int64_t)blocks(pages) * c.n_kv_heads < 1024) pages -= 8;
   a.pages = pages;
-  // n tokens touch at most n / span + 2 blocks, and no more blocks than tokens
-  const int span = pages * c.page_size;
-  const int64_t blocks = (int64_t)ch.n_tokens / span + 2ll * c.batch;
-  a.kv_wgs = (int)(blocks < ch.n_tokens ? blocks : ch.n_tokens);
+  a.kv_wgs = blocks(pages);
   a.heads_per_wg = c.n_kv_heads < 4 ? c.n_kv_heads : 4;
   while (a.heads_per_wg > 1 && (int64_t)a.kv_wgs * ((c.n_kv_heads + a.heads_per_wg - 1) / a.heads_per_wg) < 1024) a.heads_per_wg /= 2;
   while (a.heads_per_wg > 1 && a.heads_per_wg * 2 * kHeadDim * pages * 2 > 32 * 1024) a.heads_per_wg /= 2;
@@ -391,7 +410,8 @@ hipError_t launch_append_chunk(const CacheView& c, const ChunkView& ch, const Ro
   a.arrived = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + ROCKETKV_WS_HEADER_BYTES / 2);
   const size_t lds = (size_t)kBlockTokens * kHeadDim / 2 * sizeof(float2) + 2 * (size_t)kBlockTokens * kHeadDim * sizeof(bf16_t) +
                      (kmax ? (size_t)a.heads_per_wg * 2 * kHeadDim * pages * sizeof(bf16_t) : 0);
-  hipLaunchKernelGGL(append_chunk_kernel, dim3(a.kv_wgs * a.head_groups + q_wgs), dim3(kRopeT), lds, st, c, a);
+  const int n_kv = a.kv_wgs * a.head_groups;
+  hipLaunchKernelGGL(rope_is_odd(r) ? append_chunk_kernel<true> : append_chunk_kernel<false>, dim3(n_kv + q_wgs), dim3(kRopeT), lds, st, c, a);
   return hipGetLastError();
 }
 

@@ -490,19 +490,31 @@ class Rope:
         return RopeStruct(2 * int(self.inv_freq.shape[0]), int(self.interleaved), _ptr(self.inv_freq), self.scale)
 
 
+_dtypes = {}
+
+
 def _tensor(name, t, dtype, shape, rows=False):
-    """What a pointer cannot say: type, shape (None: any) and layout, contiguous or, with `rows`, in rows of any stride."""
-    import torch
-    ok = t.dtype == getattr(torch, dtype) and t.dim() == len(shape) and all(s in (None, n) for s, n in zip(shape, t.shape))
+    """What a pointer cannot say: type, shape (None: any) and layout, contiguous or, with `rows`, tokens at any stride."""
+    want = _dtypes.get(dtype)
+    if want is None:
+        import torch
+        want = _dtypes[dtype] = getattr(torch, dtype)
+    have = t.shape
+    ok = t.dtype is want and len(have) == len(shape)
+    if ok:
+        for w, h in zip(shape, have):
+            if w is not None and w != h:
+                ok = False
     if not ok:
-        raise RocketKVError(INVALID_ARG, f"{name}: need {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    if not (t.is_contiguous() or (rows and t.numel() > 0 and t[0].is_contiguous())):
+        raise RocketKVError(INVALID_ARG, f"{name}: need {dtype} {tuple(shape)}, got {t.dtype} {tuple(have)}")
+    if not t.is_contiguous() and not (rows and t.stride()[1:] == (have[2], 1)):
         raise RocketKVError(INVALID_ARG, f"{name}: inner dimensions must be contiguous")
 
 
 def _row_stride(t):
     """Elements between tokens (a single token may have any)."""
-    return int(t.stride(0)) if t.shape[0] > 1 else int(t.shape[1] * t.shape[2])
+    n, heads, channels = t.shape
+    return t.stride(0) if n > 1 else heads * channels
 
 
 def rope_frequencies(rot_dim: int, theta: float, kind: int = ROPE_PLAIN, factor: float = 1.0, low: float = 1.0,
@@ -518,8 +530,8 @@ def rope_frequencies(rot_dim: int, theta: float, kind: int = ROPE_PLAIN, factor:
 
 def rope(rope: Rope, positions, x, y, stream=None):
     """x, y: bf16 [tokens][heads][128], tokens at any stride; positions: int32 [tokens].  y may be x."""
-    n, heads = int(x.shape[0]), int(x.shape[1])
     _tensor("x", x, "bfloat16", (None, None, 128), rows=True)
+    n, heads, _ = x.shape
     _tensor("y", y, "bfloat16", (n, heads, 128), rows=True)
     _tensor("positions", positions, "int32", (n,))
     if n == 0:
