@@ -343,9 +343,8 @@ int32_t rocketkv_mt_hsa_decode_append(const rocketkv_cache_t* cache, const rocke
 /*
  * A chunk: the new tokens of all sequences of a cache, packed one behind the other.  Row r of a packed
  * tensor is one token; rows starts[b] .. starts[b+1]-1 belong to sequence b, in order.  A sequence may bring
- * no row, one, or a whole prompt.  starts is ascending from >= 0 to <= n_tokens; rows in front of starts[0] and behind
- * starts[batch] are neither read nor written.  The struct lives in host memory, starts on the device.  (Entries that
- * descend or leave [0, n_tokens] cut a sequence's rows short; no call leaves its buffers for them.)
+ * no row, one, or a whole prompt.  starts must ascend from >= 0 to <= n_tokens; rows in front of starts[0] and behind
+ * starts[batch] are neither read nor written.  The struct lives in host memory, starts on the device.
  */
 #define ROCKETKV_MAX_CHUNK (1 << 24)
 typedef struct rocketkv_chunk {
@@ -426,6 +425,7 @@ int32_t rocketkv_append_chunk(const rocketkv_cache_t* cache, const rocketkv_chun
  * q, out: bf16 [n_tokens][n_q_heads][head_dim].  out_lse: optional fp32 [n_tokens][n_q_heads], natural-log sum-exp of the
  * scaled logits.  Absent pages are skipped; a row with nothing to attend to gets zeros and -inf.
  * Keys and values of a row's future, and whatever lies where no token is, may be anything.
+ * out must not overlap q.
  * workspace: rocketkv_workspace_bytes(ROCKETKV_OP_CHUNK_ATTEND, cache, n_tokens, 0).
  */
 int32_t rocketkv_chunk_attend(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const void* q, void* out,
@@ -448,7 +448,8 @@ int32_t rocketkv_accumulate_weights(const rocketkv_cache_t* cache, const rocketk
  * Eviction by accumulated weight.  Per (sequence, KV head) of S = src->seq_lens[b] tokens: all are kept if
  * S <= keep_budget; otherwise the last n_recent tokens and, of the others, the keep_budget - n_recent with the largest
  * weight (ties: lower position; NaN counts as larger than every number).  K, V and weights of the kept tokens go to
- * `dst`, in ascending position, and dst->seq_lens[b] = min(S, keep_budget).  src is left as it is.
+ * `dst`, in ascending position, and dst->seq_lens[b] = min(S, keep_budget).  src is left as it is.  Of a kept token whose
+ * page is absent nothing moves but its weight.  A sequence longer than src counts as empty.
  * weights: fp32 [batch][n_kv_heads][src->pages_cap * src->page_size], 16-byte aligned.
  * dst: a cache with pools and lengths of its own, the same head counts, room for keep_budget tokens, any page size and
  *      V layout (channel-major: page_size 16, for src as well).

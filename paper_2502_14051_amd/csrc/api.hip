@@ -921,6 +921,7 @@ int32_t rocketkv_chunk_attend(const rocketkv_cache_t* cache, const rocketkv_chun
   const int64_t stride = (int64_t)cache->n_q_heads * kHeadDim;
   if (int r = check_rows(q, stride, cache->n_q_heads, "q", who)) return r;
   if (int r = check_rows(out, stride, cache->n_q_heads, "out", who)) return r;
+  if (q == out) return fail(ROCKETKV_INVALID_ARG, "%s: q and out must be distinct", who);
   const CacheView v = view_of(cache);
   const ChunkPlan plan = plan_chunk_attend(v, chunk->n_tokens);
   if (plan.workgroups > 2147483647ll) return fail(ROCKETKV_UNSUPPORTED, "%s: too many rows for one launch", who);

@@ -418,6 +418,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
       const uint32_t keys = use_late(key_at);
       u32x4 vf[2][4], pf[2];
       float sums[8];
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         fence();
@@ -428,6 +429,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
         pf[j / 4][j % 4] = pack_bf16x2(x, y);
       }
       fence();
+      __builtin_amdgcn_s_setprio(0);
       float sum = ((sums[0] + sums[1]) + (sums[2] + sums[3])) + ((sums[4] + sums[5]) + (sums[6] + sums[7]));
       if (__any(!(sum <= kSumLimit))) follow_maximum(S, sum, pf);
       l += sum;
@@ -546,8 +548,9 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(CacheView c, ChunkAtte
 
 ChunkPlan plan_chunk_attend(const CacheView& c, int n_tokens) {
   ChunkPlan p;
-  // 32 bits reach every row of a token-major pool below 4 GiB
-  p.far = c.v_token_major && (c.n_phys_pages * c.stride_page + kMaxGroup * kHeadDim) * (int64_t)sizeof(bf16_t) >= (int64_t)1 << 32;
+  // 32 bits reach every row of a token-major pool whose last tile ends below 4 GiB
+  const int64_t end = (c.n_phys_pages - 1) * c.stride_page + (c.n_kv_heads - 1) * c.stride_head + (int64_t)c.page_size * kHeadDim;
+  p.far = c.v_token_major && end * (int64_t)sizeof(bf16_t) >= (int64_t)1 << 32;
   // 256 rows to a workgroup share what it reads; 128 where a sequence has no more on average (not with 64-bit offsets, for
   // which the registers of that form do not suffice)
   p.tile_rows = p.far || (int64_t)n_tokens * c.group > 128ll * c.batch ? 256 : 128;

@@ -18,7 +18,7 @@ namespace rkv {
 
 constexpr int kChunkPartSteps = 6;
 constexpr int kChunkLeastSteps = 8;     // no part is smaller
-constexpr int kChunkRounds = 2;         // parts for up to so many rounds of workgroups over the chip
+constexpr int kChunkRounds = 3;         // parts for up to so many rounds of workgroups over the chip
 constexpr int kChunkWhole = 1 << 30;    // nothing is cut
 
 RKV_HD constexpr int chunk_ceil(int a, int b) { return a / b + (a % b != 0); }
@@ -32,9 +32,10 @@ struct ChunkLoad {
   int longest;  // steps of the longest
 };
 
-// Steps per part.  `slots`: workgroups the chip holds at a time; `count(size)`: workgroups at that size.  Of one round
-// and two the better is taken: 56 tiles of 2049 steps over 256 slots come as 4 parts each in one round, 87 % of it, or as
-// 9 in two, 98 %.  The result never needs more than max(tiles, slots * kChunkRounds) workgroups.
+// Steps per part.  `slots`: workgroups the chip holds at a time; `count(size)`: workgroups at that size.  Of one to three
+// rounds the best is taken: 56 tiles of 2049 steps over 256 slots come as 4 parts each in one round, 87 % of it, or as 9 in
+// two, 98 %; 171 to 192 tiles gain nothing by halves in two rounds, but by quarters in three.  The result never needs more
+// than max(tiles, slots * kChunkRounds) workgroups.
 template <class Count>
 RKV_HD inline int chunk_part_size(const ChunkLoad& load, int slots, const Count& count) {
   if (load.tiles >= slots * kChunkRounds || load.longest <= kChunkLeastSteps) return kChunkWhole;

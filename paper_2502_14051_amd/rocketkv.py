@@ -493,6 +493,11 @@ class Rope:
 _dtypes = {}
 
 
+def _current_device():
+    import torch
+    return torch.cuda.current_device()
+
+
 def _tensor(name, t, dtype, shape, rows=False):
     """What a pointer cannot say: type, shape (None: any) and layout, contiguous or, with `rows`, tokens at any stride."""
     want = _dtypes.get(dtype)
@@ -507,6 +512,9 @@ def _tensor(name, t, dtype, shape, rows=False):
                 ok = False
     if not ok:
         raise RocketKVError(INVALID_ARG, f"{name}: need {dtype} {tuple(shape)}, got {t.dtype} {tuple(have)}")
+    device = t.get_device()
+    if device < 0 or device != _current_device():
+        raise RocketKVError(INVALID_ARG, f"{name}: on {t.device}, not on the current GPU")
     if not t.is_contiguous() and not (rows and t.stride()[1:] == (have[2], 1)):
         raise RocketKVError(INVALID_ARG, f"{name}: inner dimensions must be contiguous")
 

@@ -190,3 +190,37 @@ def test_many_sequences_and_graph():
         assert torch.equal(kmax, omax) and torch.equal(kmin, omin) and torch.equal(c.cache.seq_lens, other.seq_lens)
         assert torch.equal(q_out, oq)
     assert c.cache.seq_lens.tolist() == [(7 * b) % 50 + 4 * (b % 4) for b in range(B)]
+
+
+def test_tensors_of_another_kind_are_refused():
+    x = torch.zeros((3, 4, 128), dtype=torch.bfloat16, device="cuda")
+    pos, r = torch.zeros(3, dtype=torch.int32, device="cuda"), rk.Rope(freq(128))
+    wide = torch.zeros((3, 4, 256), dtype=torch.bfloat16, device="cuda")
+    for a, b, p, needle in ((x, x[:2], pos, "y"), (x, x, pos.long(), "int32"), (x, x.cpu(), pos, "y: on"), (x, x, pos[:2], "positions"),
+                            (wide[..., :128], x, pos, "contiguous"), (x.transpose(0, 1), x, pos, "contiguous")):
+        with pytest.raises(rk.RocketKVError) as e:
+            rk.rope(r, p, a, b)
+        assert e.value.status == rk.INVALID_ARG and needle in str(e.value)
+    c = ref.Case(25, [3, 4], [1, 2], 4, 2)
+    q, k, v = new_rows(c, 5)
+    kmax, kmin = rk.alloc_summaries(c.cache)
+    ws = rk.alloc_workspace(rk.OP_APPEND_CHUNK, c.cache, c.rows)
+    for args, kw in (((k[:2], v, kmax, kmin), {}), ((k, v[:, :1], kmax, kmin), {}), ((k, v, kmax[..., :1], kmin), {}),
+                     ((k, v, kmax, None), {}), ((k, v, kmax, kmin), dict(q=q)), ((k, v, kmax, kmin), dict(q=q, q_out=q[:, :2])),
+                     ((k, v, kmax, kmin), dict(positions=torch.zeros(3, dtype=torch.int32, device="cuda")))):
+        with pytest.raises(rk.RocketKVError):
+            rk.append_chunk(c.cache, c.chunk, *args, ws, **kw)
+    with pytest.raises(rk.RocketKVError):
+        rk.append_chunk(c.cache, rk.Chunk(c.chunk.starts[:2], c.rows), k, v, kmax, kmin, ws)
+    with pytest.raises(rk.RocketKVError):
+        rk.append_chunk(c.cache, c.chunk, k, v, kmax, kmin, ws[:1024])
+
+
+def test_no_tokens_at_all():
+    c = ref.Case(26, [5, 9], [0, 0], 4, 2)
+    kmax, kmin = rk.alloc_summaries(c.cache)
+    none = lambda h: torch.empty((0, h, 128), dtype=torch.bfloat16, device="cuda")
+    rk.append_chunk(c.cache, c.chunk, none(2), none(2), kmax, kmin, rk.alloc_workspace(rk.OP_APPEND_CHUNK, c.cache, 0))
+    rk.rope(rk.Rope(freq(128)), torch.empty(0, dtype=torch.int32, device="cuda"), none(4), none(4))
+    rk.chunk_attend(c.cache, c.chunk, none(4), none(4), None, rk.alloc_workspace(rk.OP_CHUNK_ATTEND, c.cache, 0))
+    assert c.cache.seq_lens.tolist() == [5, 9]

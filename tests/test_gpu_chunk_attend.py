@@ -137,22 +137,39 @@ def test_future_values_that_are_not_finite(ps, token_major, bad, lens, news):
             assert torch.equal(out[row][:, ~hit], clean[row][:, ~hit]), f"sequence {b}, row {i}"
 
 
-def test_pool_beyond_32_bits():
-    """Rows of a token-major pool of more than 4 GiB, at its far end too."""
-    c = ref.Case(17, [500, 70], [100, 1], 8, 2, 16, True, shuffled=False)
-    out, lse = attend(c)
+@pytest.mark.parametrize("token_major", [False, True])
+def test_pools_beyond_32_bits(token_major):
+    """All of the operators over pools of more than 4 GiB, at their far ends too, beside small pools of the same tokens."""
+    c = ref.Case(17, [500, 70], [100, 1], 8, 2, 16, token_major, shuffled=False, spare_pages=16)
+    small = c.cache
     pages = (5 << 30) // (2 * 16 * 128 * 2)
-    big = rk.alloc_cache(2, 8, 2, 128, 16, c.cache.pages_cap, "cuda", n_phys_pages=pages, v_layout=rk.V_TOKEN_MAJOR)
-    table = torch.randperm(pages, generator=torch.Generator().manual_seed(0))[:2 * big.pages_cap]
-    table[0], table[1], table[40] = pages - 1, 0, pages - 2
-    big.block_table = table.reshape(2, -1).to(torch.int32).cuda()
+    table = torch.randperm(pages, generator=torch.Generator().manual_seed(0))[:2 * small.pages_cap]
+    table[0], table[1], table[35], table[40] = pages - 1, 0, pages - 3, pages - 2
+    assert len(set(table.tolist())) == len(table)
+    big = rk.alloc_cache(2, 8, 2, 128, 16, small.pages_cap, "cuda", block_table=table.reshape(2, -1).to(torch.int32).cuda(),
+                         n_phys_pages=pages, v_layout=small.v_layout)
     at = table.cuda()
-    big.k_pool[at], big.v_pool[at] = c.cache.k_pool[:len(at)], c.cache.v_pool[:len(at)]
-    big.seq_lens.copy_(c.cache.seq_lens)
-    c.cache = big
-    far, far_lse = attend(c)
-    assert torch.equal(far[c.rows_of(0)], out[c.rows_of(0)])
-    ref.check_attention(c, far, far_lse)
+    big.k_pool[at], big.v_pool[at] = small.k_pool[:len(at)], small.v_pool[:len(at)]
+    big.seq_lens.copy_(small.seq_lens)
+    r = rk.Rope(torch.ones(64, dtype=torch.float64, device="cuda") / 100)
+    results = []
+    for cache in (small, big):
+        kmax, kmin = rk.alloc_summaries(cache)
+        rk.build_page_summaries(cache, kmax, kmin)
+        k = torch.randn((c.rows, 2, 128), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+        rk.append_chunk(cache, c.chunk, k, k, kmax, kmin, rk.alloc_workspace(rk.OP_APPEND_CHUNK, cache, c.rows), rope=r)
+        c.cache = cache
+        out, lse = attend(c)
+        w = rk.alloc_weights(cache)
+        rk.accumulate_weights(cache, c.chunk, c.q, lse, None, w)
+        dst = rk.alloc_cache(2, 8, 2, 128, 16, 16, "cuda", zero=True, v_layout=cache.v_layout)
+        rk.weight_evict(cache, w, 8, 200, dst, None, None, rk.alloc_workspace(rk.OP_WEIGHT_EVICT, cache, 8, 200))
+        results.append([kmax, kmin, cache.seq_lens, out, lse, w, dst.k_pool, dst.v_pool, dst.seq_lens])
+    for i, (a, b) in enumerate(zip(*results)):
+        assert torch.equal(a, b), f"result {i}"
+    K, V = rk.unpack_cache(small)
+    c.K, c.V, c.lens = K, V, [n + m for n, m in zip(c.lens, c.news)]
+    ref.check_attention(c, *results[1][3:5])
 
 
 def test_more_new_tokens_than_the_cache_holds():
