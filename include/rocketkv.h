@@ -426,7 +426,8 @@ int32_t rocketkv_append_chunk(const rocketkv_cache_t* cache, const rocketkv_chun
  * scaled logits.  Absent pages are skipped; a row with nothing to attend to gets zeros and -inf.
  * Keys and values of a row's future, and whatever lies where no token is, may be anything.
  * out must not overlap q.
- * workspace: rocketkv_workspace_bytes(ROCKETKV_OP_CHUNK_ATTEND, cache, n_tokens, 0).
+ * workspace: rocketkv_workspace_bytes(ROCKETKV_OP_CHUNK_ATTEND, cache, n_tokens, 0): 98 MiB for any n_tokens >= 1, so one
+ * serves calls of any size.
  */
 int32_t rocketkv_chunk_attend(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const void* q, void* out,
                               float* out_lse, void* workspace, size_t workspace_bytes, void* stream);

@@ -2,7 +2,7 @@
 // of a prompt, a turn, drafted tokens, single tokens, in any mixture.
 //
 // Rows of a (sequence, KV head) are its new tokens times the group's query heads, so every key serves the whole group.
-// A workgroup takes a tile of rows, 32 or 64 to a wavefront, and walks the keys 64 at a time through LDS, one pass with
+// A workgroup takes a tile of rows, 32 to a wavefront, and walks the keys 64 at a time through LDS, one pass with
 // the running maximum m and sum l of each row:
 //
 //   S^T[key][row]     = K[key][:] . Q[row][:]              A = keys (32 rows), B = queries, kept in registers
@@ -12,7 +12,7 @@
 // outputs never leave it, but for one exchange with the lane 32 further, which holds the same row's other keys.  The
 // product leaves a lane the keys of A's rows 8a + 4h + r; with the rows of K read in an order that swaps bits 2 and 3,
 // these are keys 16x + 8h + 0..7, which packed to bf16 are the second product's operand as they stand.  P is rounded to
-// bf16 there (relative 2^-9 at most each, the sum l takes the unrounded values); everything else is fp32.
+// bf16 there (relative 2^-8 at most each, the sum l takes the unrounded values); everything else is fp32.
 #include <type_traits>
 
 #include "attend_core.h"
@@ -84,14 +84,15 @@ struct ChunkAttendArgs {
   float* out_lse;
   float* partial;     // [workgroup][rows][128] sums of the parts; null: no tile is ever cut
   float2* part_stats; // [workgroup][rows] their maxima and sums of exponentials
+  int4* part_place;   // [workgroup] what the merge needs: first row in the packed tensors, rows and part, parts, ChunkPlace::next
   int tile_tokens;    // tokens of a row tile
-  int slots;          // workgroups the chip holds at a time
+  int slots, most;    // workgroups the chip holds at a time; parts at most
 };
 
 // Where a workgroup works: tile `tile` of sequence b, part `part` of `parts` of its keys.
 struct ChunkPlace {
   int b, tile, part, parts;
-  int first;  // index of the tile's first part among all parts of a KV head
+  int first, next;  // indexes among all parts of a KV head: of the tile's first part, and how much further each other is
 };
 
 struct ChunkSeq {
@@ -126,10 +127,10 @@ __device__ __forceinline__ int chunk_size_for(const CacheView& c, const ChunkAtt
   each([&](int t, int steps) {
     load.tiles += total(t) * c.n_kv_heads;
     // (a coarser count keeps the sums in range where sequences are long: 2^15 steps are 2^21 tokens)
-    load.work += (float)total(min(t, a.slots * kChunkRounds) * min(steps, 1 << 15)) * (float)c.n_kv_heads;
+    load.work += (float)total(min(t, a.most) * min(steps, 1 << 15)) * (float)c.n_kv_heads;
     load.longest = max(load.longest, (int)wave_max_u32((uint32_t)steps));
   });
-  return chunk_part_size(load, a.slots, [&](int size) {
+  return chunk_part_size(load, a.slots, a.most, [&](int size) {
     int n = 0;
     each([&](int t, int steps) { n += total(t * chunk_parts(steps, size)); });
     return n * c.n_kv_heads;
@@ -145,10 +146,11 @@ __device__ __forceinline__ bool chunk_place(const CacheView& c, const ChunkAtten
     return false;
   const ChunkSeq s = chunk_seq(c, a.ch, p.b);
   p.parts = chunk_parts(chunk_ceil(s.len, kStep), size);
-  const int tiles = chunk_ceil(s.n, a.tile_tokens);
-  p.part = idx % p.parts;
-  p.first = at - p.part;
-  p.tile = tiles - 1 - idx / p.parts;  // the tiles that see most come first
+  // the tiles of one part side by side, as they read the same keys; those that see most first
+  p.next = chunk_ceil(s.n, a.tile_tokens);
+  p.part = idx / p.next;
+  p.tile = p.next - 1 - idx % p.next;
+  p.first = at - p.part * p.next;
   return true;
 }
 
@@ -162,12 +164,18 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
   const int col = lane % 32, h = lane / 32;
   const int g = blockIdx.x % c.n_kv_heads, at = blockIdx.x / c.n_kv_heads;
   ChunkPlace pl;
-  if (!chunk_place(c, a, chunk_size_for(c, a), at, pl)) return;
-  if (pl.parts > 1 && (int)blockIdx.x >= a.slots * kChunkRounds) return;  // (`starts` that overlap: no place for its rows)
+  const bool any = chunk_place(c, a, chunk_size_for(c, a), at, pl);
+  const bool holds = a.partial && (int)blockIdx.x < a.most;  // a place for a part's rows
+  if (!any) {
+    if (holds && threadIdx.x == 0) a.part_place[blockIdx.x] = make_int4(0, 0, 1, 0);
+    return;
+  }
+  if (pl.parts > 1 && !holds) return;  // (`starts` that overlap)
   const ChunkSeq s = chunk_seq(c, a.ch, pl.b);
   const int G = c.group, ps = c.page_size;
   const int t0 = pl.tile * a.tile_tokens, nt = min(a.tile_tokens, s.n - t0);
   const int rows = nt * G;
+  if (holds && threadIdx.x == 0) a.part_place[blockIdx.x] = make_int4(s.row + t0, rows << 16 | pl.part, pl.parts, pl.next);
   const int pos0 = s.len - s.n + t0;  // place in the cache of the tile's first token
 
   // the part's steps
@@ -495,28 +503,29 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
   if (a.out_lse && h == 0) a.out_lse[row] = sum > 0.f ? (m + __log2f(sum)) * kLn2 : -INFINITY;
 }
 
-// The parts of a tile joined: a wavefront per row, a lane per two channels.
-__global__ __launch_bounds__(256) void chunk_merge_kernel(CacheView c, ChunkAttendArgs a, int tile_rows) {
-  const int g = blockIdx.x % c.n_kv_heads, at = blockIdx.x / c.n_kv_heads;
-  const int size = chunk_size_for(c, a);
-  if (size == kChunkWhole) return;
-  ChunkPlace pl;
-  if (!chunk_place(c, a, size, at, pl) || pl.parts == 1) return;
-  const ChunkSeq s = chunk_seq(c, a.ch, pl.b);
-  const int G = c.group, t0 = pl.tile * a.tile_tokens, rows = min(a.tile_tokens, s.n - t0) * G;
+constexpr int kMergeWaves = 8, kMergeSlices = 2;  // wavefronts to a workgroup, workgroups to a part
+
+// The parts of a tile joined: a wavefront per row, a lane per two channels.  A row is a chain of dependent reads, so it is
+// wavefronts at work that count: 16 per part were 2 to 35 % of a whole call better than 4.
+__global__ __launch_bounds__(kMergeWaves * kWave) void chunk_merge_kernel(CacheView c, ChunkAttendArgs a, int tile_rows) {
+  const int4 place = a.part_place[blockIdx.x];
+  const int parts = place.z;
+  if (parts == 1) return;
+  const int g = blockIdx.x % c.n_kv_heads, at = blockIdx.x / c.n_kv_heads, G = c.group;
+  const int rows = place.y >> 16, part = place.y & 0xffff, first = at - part * place.w;
   const int lane = threadIdx.x % kWave;
-  const int64_t next = (int64_t)c.n_kv_heads * tile_rows;  // rows from part to part
+  const int64_t next = (int64_t)place.w * c.n_kv_heads * tile_rows;  // rows from part to part
   // the tile's parts share its rows
-  for (int r = pl.part + pl.parts * (threadIdx.x / kWave); r < rows; r += pl.parts * 4) {
-    const int64_t row0 = ((int64_t)pl.first * c.n_kv_heads + g) * tile_rows + r;
+  for (int r = part + parts * (threadIdx.x / kWave + kMergeWaves * blockIdx.y); r < rows; r += parts * kMergeWaves * kMergeSlices) {
+    const int64_t row0 = ((int64_t)first * c.n_kv_heads + g) * tile_rows + r;
     const float* p = a.partial + row0 * kHeadDim;
     const float2* stats = a.part_stats + row0;
     float m = kNegBig;
-    for (int i = lane; i < pl.parts; i += kWave) m = fmaxf(m, stats[i * next].x);
+    for (int i = lane; i < parts; i += kWave) m = fmaxf(m, stats[i * next].x);
     m = wave_max_f32(m);
     float l = 0.f, x = 0.f, y = 0.f;
-    for (int i0 = 0; i0 < pl.parts; i0 += kWave) {
-      const int n = min(kWave, pl.parts - i0);
+    for (int i0 = 0; i0 < parts; i0 += kWave) {
+      const int n = min(kWave, parts - i0);
       float w = 0.f;
       if (lane < n) {
         const float2 ml = stats[(i0 + lane) * next];
@@ -539,7 +548,7 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(CacheView c, ChunkAtte
 #pragma unroll
     for (int d = 1; d < kWave; d *= 2) l += __shfl_xor(l, d);
     const int t = r / G;
-    const int64_t row = (int64_t)(s.row + t0 + t) * c.n_q_heads + (int64_t)g * G + r - t * G;
+    const int64_t row = (int64_t)(place.x + t) * c.n_q_heads + (int64_t)g * G + r - t * G;
     const float inv = l > 0.f ? 1.f / l : 0.f;
     *reinterpret_cast<uint32_t*>(a.out + row * kHeadDim + 2 * lane) = pack_bf16x2(x * inv, y * inv);
     if (a.out_lse && lane == 0) a.out_lse[row] = l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
@@ -556,14 +565,16 @@ ChunkPlan plan_chunk_attend(const CacheView& c, int n_tokens) {
   p.tile_rows = p.far || (int64_t)n_tokens * c.group > 128ll * c.batch ? 256 : 128;
   p.tile_tokens = p.tile_rows / c.group;
   p.slots = 256 * (256 / p.tile_rows);
-  const int64_t most = (int64_t)p.slots * kChunkRounds;
   const int64_t at_least = ((int64_t)n_tokens + p.tile_tokens - 1) / p.tile_tokens * c.n_kv_heads;
   int64_t tiles = (int64_t)n_tokens / p.tile_tokens + c.batch;
   if (tiles > n_tokens) tiles = n_tokens;
   tiles *= c.n_kv_heads;
-  p.cuts = at_least < most;
-  p.workgroups = p.cuts && tiles < most ? most : tiles;
-  p.total_bytes = p.cuts ? (size_t)ROCKETKV_WS_HEADER_BYTES + (size_t)most * p.tile_rows * (kHeadDim + 2) * sizeof(float) : 0;
+  const int rounds = chunk_rounds(at_least, p.slots);
+  p.most = p.slots * rounds;
+  p.cuts = at_least < p.most;
+  p.workgroups = p.cuts && tiles < p.most ? p.most : tiles;
+  // (for any number of tokens, so that what serves many serves few)
+  p.total_bytes = n_tokens ? (size_t)ROCKETKV_WS_HEADER_BYTES + (size_t)256 * kChunkRounds * (256 * (kHeadDim + 2) * sizeof(float) + 2 * sizeof(int4)) : 0;
   return p;
 }
 
@@ -576,9 +587,11 @@ hipError_t launch_chunk_attend(const CacheView& c, const ChunkView& ch, const bf
   a.out = out;
   a.out_lse = out_lse;
   a.partial = plan.cuts ? reinterpret_cast<float*>(static_cast<char*>(ws) + ROCKETKV_WS_HEADER_BYTES) : nullptr;
-  a.part_stats = reinterpret_cast<float2*>(a.partial + (int64_t)plan.slots * kChunkRounds * plan.tile_rows * kHeadDim);
+  a.part_stats = reinterpret_cast<float2*>(a.partial + (int64_t)plan.most * plan.tile_rows * kHeadDim);
+  a.part_place = reinterpret_cast<int4*>(a.part_stats + (int64_t)plan.most * plan.tile_rows);
   a.tile_tokens = plan.tile_tokens;
   a.slots = plan.slots;
+  a.most = plan.most;
   const auto launch = [&](auto kernel, int waves) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)plan.workgroups), dim3(waves * kWave), 4 * kKeyBytes, st, c, a);
   };
@@ -588,7 +601,7 @@ hipError_t launch_chunk_attend(const CacheView& c, const ChunkView& ch, const bf
   else if (c.v_token_major) launch(chunk_attend_kernel<true, false, 4>, 4);
   else launch(chunk_attend_kernel<false, false, 4>, 4);
   if (plan.cuts) {
-    hipLaunchKernelGGL(chunk_merge_kernel, dim3(plan.slots * kChunkRounds), dim3(256), 0, st, c, a, plan.tile_rows);
+    hipLaunchKernelGGL(chunk_merge_kernel, dim3(plan.most, kMergeSlices), dim3(kMergeWaves * kWave), 0, st, c, a, plan.tile_rows);
   }
   return hipGetLastError();
 }

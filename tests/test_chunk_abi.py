@@ -137,7 +137,8 @@ def test_workspace_sizes(L):
     size = lambda op, a, b=0, **kw: L.rocketkv_workspace_bytes(op, C.byref(cache(**kw)), a, b)
     assert size(rk.OP_APPEND_CHUNK, 0) == size(rk.OP_APPEND_CHUNK, 1 << 20) == 65536
     assert size(rk.OP_CHUNK_ATTEND, 1) > 65536
-    assert size(rk.OP_CHUNK_ATTEND, 1 << 20) == 0 and rk.last_error() == ""  # every tile whole: none is needed
+    assert size(rk.OP_CHUNK_ATTEND, 0) == 0 and rk.last_error() == ""
+    assert size(rk.OP_CHUNK_ATTEND, 1 << 20) == size(rk.OP_CHUNK_ATTEND, 1)  # what serves many tokens serves few
     for op in (rk.OP_APPEND_CHUNK, rk.OP_CHUNK_ATTEND):
         assert size(op, -1) == 0 and "n_tokens" in rk.last_error()
         assert size(op, rk.MAX_CHUNK + 1) == 0 and "exceeds" in rk.last_error()
