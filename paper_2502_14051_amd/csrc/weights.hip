@@ -49,26 +49,32 @@ struct WeightArgs {
   float* w_out;
 };
 
-// A wavefront holds 64 keys.  Two take the first 64 rows of a step, two the same keys and the other 64: a workgroup is done
-// with 128 keys in half the time that four wavefronts of keys of their own take for 256, and the last ones of a launch leave
-// less of the chip idle (2048 tokens of 32 heads over 34816 keys and 8 KV heads, us: 673 with 256 keys, two and an eighth
-// rounds of workgroups over the chip; 644 so; eight wavefronts and 256 keys, one workgroup to a compute unit, 705; 32 keys to
-// a wavefront 743).  A unit is 32 rows; its exponentials stand beside the next unit's products, as in the attention, so in
-// step `it` the rows of step it + 1 are read.
-constexpr int NK = 2;  // blocks of 32 keys to a wavefront
-__global__ __launch_bounds__(kWeightWaves * kWave) __attribute__((amdgpu_waves_per_eu(2)))
-void weights_kernel(CacheView c, WeightArgs a) {
-  __shared__ __align__(256) unsigned char s_q[2][kRowStepBytes];  // [128 rows][16 chunks], chunk x of row r at x ^ r % 16
-  __shared__ __align__(16) float s_lse[4][kRowStep];              // in the log2 domain; +inf: a row that adds nothing
-  __shared__ float s_sum[kKeyWaves * 32 * NK];
-  constexpr int kKeys = kKeyWaves * 32 * NK;
+constexpr int kTileKeys = kKeyWaves * 64, kWeightSlots = 512;  // keys of a workgroup; workgroups the chip holds at a time
+
+__device__ __forceinline__ int weight_len(const CacheView& c, int b) {
+  const int n = c.seq_lens[b];
+  return n < 0 ? 0 : min(n, c.pages_cap * c.page_size);
+}
+
+// A wavefront holds NK blocks of 32 keys.  Two take the first 64 rows of a step, two the same keys and the other 64: a
+// workgroup is done with 128 keys in half the time that four wavefronts of keys of their own take for 256, and the last
+// ones of a launch leave less of the chip idle.  A unit is 32 rows; its exponentials stand beside the next unit's
+// products, as in the attention, so in step `it` the rows of step it + 1 are read.
+struct WeightShared {
+  __align__(256) unsigned char q[2][kRowStepBytes];  // [128 rows][16 chunks], chunk x of row r at x ^ r % 16
+  __align__(16) float lse[4][kRowStep];              // in the log2 domain; +inf: a row that adds nothing
+  float sum[kTileKeys];
+};
+template <int NK>
+__device__ __forceinline__ void weights_of_keys(const CacheView& c, const WeightArgs& a, WeightShared& sh, int b, int g, int key0) {
+  auto& s_q = sh.q;
+  auto& s_lse = sh.lse;
+  auto& s_sum = sh.sum;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int col = lane % 32, h = lane / 32;
   const int kw = wave % kKeyWaves, own_rows = wave / kKeyWaves * 64;  // which 64 keys, and where in a step its rows begin
-  const int unit = blockIdx.y, b = unit / c.n_kv_heads, g = unit % c.n_kv_heads;
   const int G = c.group, ps = c.page_size, cap = c.pages_cap * ps;
-  const int n_now = c.seq_lens[b], len = n_now < 0 ? 0 : min(n_now, cap);
-  const int key0 = blockIdx.x * kKeys;
+  const int len = weight_len(c, b);
   if (key0 >= len) return;
   const int row0 = chunk_first(a.ch, b), n = chunk_rows(a.ch, b);
   const int old = len - n;  // place in the cache of the first new token (the first ones see nothing if it is negative)
@@ -210,10 +216,39 @@ void weights_kernel(CacheView c, WeightArgs a) {
   for (int x = 0; x < NK; ++x) {
     const int at_key = (kw * NK + x) * 32 + here, key = key0 + at_key;
     if (key >= len) continue;
-    const int64_t at = (int64_t)unit * cap + key;
+    const int64_t at = ((int64_t)b * c.n_kv_heads + g) * cap + key;
     const float before = a.w_in && key < old ? a.w_in[at] : 0.f;
     a.w_out[at] = phys_page(c, b, key / ps) >= 0 ? before + (sum[x] + s_sum[at_key]) : before;
   }
+}
+
+// Tiles of 128 keys of all sequences and KV heads, the KV head running fastest: a chiplet's L2 then holds the queries of
+// one head, if there are as many.  What the last round of workgroups over the chip leaves idle, if that is half of it or
+// more, halves of the last tiles fill (us, without and with: 2048 tokens of 32 heads over 34816 keys and 8 KV heads, four
+// and a quarter rounds, 625 and 598, 0.95 PFLOP/s; 1186 tokens of 64 heads over 2242, a quarter of a round, 123 and 77).
+// Other tiles took longer: 256 keys to a workgroup of four wavefronts 673, to one of eight 705, half tiles only 743.
+__global__ __launch_bounds__(kWeightWaves * kWave) __attribute__((amdgpu_waves_per_eu(2)))
+void weights_kernel(CacheView c, WeightArgs a) {
+  __shared__ WeightShared sh;
+  const int lane = threadIdx.x % kWave;
+  const auto tiles_of = [&](int b) { return (weight_len(c, b) + kTileKeys - 1) / kTileKeys; };
+  int tiles = 0;
+  for (int b0 = 0; b0 < c.batch; b0 += kWave)
+    tiles += __builtin_amdgcn_readlane((int)wave_incl_scan(b0 + lane < c.batch ? (uint32_t)tiles_of(b0 + lane) : 0u), kWave - 1);
+  tiles *= c.n_kv_heads;
+  const int last = tiles % kWeightSlots, halved = last <= kWeightSlots / 2 ? last : 0;
+  int i = blockIdx.x, half = -1;
+  if (i >= tiles - halved) {
+    i -= tiles - halved;
+    if (i >= 2 * halved) return;
+    half = i >= halved;
+    i = tiles - halved + (half ? i - halved : i);
+  }
+  int b, tile;
+  if (!locate_tile(c.batch, i / c.n_kv_heads, tiles_of, b, tile)) return;
+  const int g = i % c.n_kv_heads;
+  if (half < 0) weights_of_keys<2>(c, a, sh, b, g, tile * kTileKeys);
+  else weights_of_keys<1>(c, a, sh, b, g, tile * kTileKeys + half * (kTileKeys / 2));
 }
 
 // For few rows, where reading the keys once is all there is to it: a wavefront for 32 keys, nothing shared, five times the
@@ -286,10 +321,9 @@ hipError_t launch_weights(const CacheView& c, const ChunkView& ch, const bf16_t*
   a.lse = lse;
   a.w_in = w_in;
   a.w_out = w_out;
-  const int units = c.batch * c.n_kv_heads, cap = c.pages_cap * c.page_size;
-  const auto grid = [&](int keys) { return dim3((unsigned)((cap + keys - 1) / keys), (unsigned)units); };
-  if ((int64_t)ch.n_tokens * c.group <= 32ll * c.batch) hipLaunchKernelGGL(weights_few_kernel, grid(128), dim3(kFewT), 0, st, c, a);
-  else hipLaunchKernelGGL(weights_kernel, grid(kKeyWaves * 32 * NK), dim3(kWeightWaves * kWave), 0, st, c, a);
+  const unsigned units = (unsigned)(c.batch * c.n_kv_heads), tiles = (unsigned)((c.pages_cap * c.page_size + kTileKeys - 1) / kTileKeys);
+  if ((int64_t)ch.n_tokens * c.group <= 32ll * c.batch) hipLaunchKernelGGL(weights_few_kernel, dim3(tiles, units), dim3(kFewT), 0, st, c, a);
+  else hipLaunchKernelGGL(weights_kernel, dim3(tiles * units + kWeightSlots / 2), dim3(kWeightWaves * kWave), 0, st, c, a);
   return hipGetLastError();
 }
 
