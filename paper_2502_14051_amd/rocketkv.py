@@ -494,8 +494,8 @@ _dtypes = {}
 
 
 def _current_device():
-    import torch
-    return torch.cuda.current_device()
+    import torch  # (where a tensor lies on a GPU, torch.cuda.current_device has nothing left to initialise)
+    return torch._C._cuda_getDevice()
 
 
 def _tensor(name, t, dtype, shape, rows=False):
@@ -505,11 +505,7 @@ def _tensor(name, t, dtype, shape, rows=False):
         import torch
         want = _dtypes[dtype] = getattr(torch, dtype)
     have = t.shape
-    ok = t.dtype is want and len(have) == len(shape)
-    if ok:
-        for w, h in zip(shape, have):
-            if w is not None and w != h:
-                ok = False
+    ok = t.dtype is want and (have == shape or len(have) == len(shape) and all(w is None or w == h for w, h in zip(shape, have)))
     if not ok:
         raise RocketKVError(INVALID_ARG, f"{name}: need {dtype} {tuple(shape)}, got {t.dtype} {tuple(have)}")
     device = t.get_device()
