@@ -924,7 +924,7 @@ int32_t rocketkv_chunk_attend(const rocketkv_cache_t* cache, const rocketkv_chun
   if (q == out) return fail(ROCKETKV_INVALID_ARG, "%s: q and out must be distinct", who);
   const CacheView v = view_of(cache);
   const ChunkPlan plan = plan_chunk_attend(v, chunk->n_tokens);
-  if (plan.workgroups > 2147483647ll) return fail(ROCKETKV_UNSUPPORTED, "%s: too many rows for one launch", who);
+  if (plan.workgroups * 512 > 0xffffffffll) return fail(ROCKETKV_UNSUPPORTED, "%s: too many rows for one launch", who);
   if (int r = check_workspace(workspace, workspace_bytes, plan.total_bytes, who)) return r;
   const hipError_t e = launch_chunk_attend(v, chunk_of(chunk), static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out),
                                            out_lse, workspace, plan, static_cast<hipStream_t>(stream));
@@ -942,6 +942,8 @@ int32_t rocketkv_accumulate_weights(const rocketkv_cache_t* cache, const rocketk
     if (int r = check_rows(q, (int64_t)cache->n_q_heads * kHeadDim, cache->n_q_heads, "q", who)) return r;
     if (!lse) return fail(ROCKETKV_INVALID_ARG, "%s: lse must not be NULL", who);
   }
+  if (weights_workgroups(view_of(cache)) * 256 > 0xffffffffll)
+    return fail(ROCKETKV_UNSUPPORTED, "%s: too many keys for one launch", who);
   const hipError_t e = launch_weights(view_of(cache), chunk_of(chunk), static_cast<const bf16_t*>(q), lse, weights_in,
                                       weights_out, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);

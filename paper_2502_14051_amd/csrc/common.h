@@ -410,6 +410,7 @@ struct ChunkPlan {
 ChunkPlan plan_chunk_attend(const CacheView& c, int n_tokens);
 hipError_t launch_chunk_attend(const CacheView& c, const ChunkView& ch, const bf16_t* q, bf16_t* out, float* out_lse,
                                void* ws, const ChunkPlan& plan, hipStream_t st);
+int64_t weights_workgroups(const CacheView& c);  // at most
 hipError_t launch_weights(const CacheView& c, const ChunkView& ch, const bf16_t* q, const float* lse, const float* w_in,
                           float* w_out, hipStream_t st);
 struct EvictPlan {

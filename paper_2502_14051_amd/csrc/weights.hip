@@ -313,6 +313,10 @@ void weights_few_kernel(CacheView c, WeightArgs a) {
   if (h == 0 && key < len) a.w_out[(int64_t)unit * cap + key] = pp >= 0 ? before + total : before;
 }
 
+int64_t weights_workgroups(const CacheView& c) {
+  return ((int64_t)c.pages_cap * c.page_size + kTileKeys - 1) / kTileKeys * c.batch * c.n_kv_heads + kWeightSlots / 2;
+}
+
 hipError_t launch_weights(const CacheView& c, const ChunkView& ch, const bf16_t* q, const float* lse, const float* w_in,
                           float* w_out, hipStream_t st) {
   WeightArgs a;
@@ -323,7 +327,7 @@ hipError_t launch_weights(const CacheView& c, const ChunkView& ch, const bf16_t*
   a.w_out = w_out;
   const unsigned units = (unsigned)(c.batch * c.n_kv_heads), tiles = (unsigned)((c.pages_cap * c.page_size + kTileKeys - 1) / kTileKeys);
   if ((int64_t)ch.n_tokens * c.group <= 32ll * c.batch) hipLaunchKernelGGL(weights_few_kernel, dim3(tiles, units), dim3(kFewT), 0, st, c, a);
-  else hipLaunchKernelGGL(weights_kernel, dim3(tiles * units + kWeightSlots / 2), dim3(kWeightWaves * kWave), 0, st, c, a);
+  else hipLaunchKernelGGL(weights_kernel, dim3((unsigned)weights_workgroups(c)), dim3(kWeightWaves * kWave), 0, st, c, a);
   return hipGetLastError();
 }
 

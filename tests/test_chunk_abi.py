@@ -98,6 +98,8 @@ ATTEND = dict(cache=cache(), chunk=chunk(), q=Q, out=OUT, lse=LSE, ws=WS, wsb=BI
     (dict(q=None), rk.INVALID_ARG, "q must not"), (dict(out=OUT + 2), rk.INVALID_ARG, "out must be"),
     (dict(out=Q), rk.INVALID_ARG, "distinct"), (dict(ws=None), rk.WORKSPACE_TOO_SMALL, "workspace"),
     (dict(wsb=1000), rk.WORKSPACE_TOO_SMALL, "workspace"), (dict(ws=WS + 8), rk.INVALID_ARG, "aligned"),
+    (dict(cache=cache(n_q_heads=256, n_kv_heads=16, stride_page=16 * 2048), chunk=chunk(n_tokens=rk.MAX_CHUNK)), rk.UNSUPPORTED, "too many rows"),
+    (dict(cache=cache(n_q_heads=136)), rk.UNSUPPORTED, "group size"),
 ])
 def test_attend_refusals(L, kw, status, needle):
     a = dict(ATTEND, **kw)
@@ -107,6 +109,7 @@ def test_attend_refusals(L, kw, status, needle):
 @pytest.mark.parametrize("kw,status,needle", [
     (dict(cache=None), rk.INVALID_ARG, "cache is NULL"), (dict(chunk=None), rk.INVALID_ARG, "chunk is NULL"),
     (dict(q=None), rk.INVALID_ARG, "q must not"), (dict(lse=None), rk.INVALID_ARG, "lse"), (dict(out=None), rk.INVALID_ARG, "weights_out"),
+    (dict(cache=cache(block_table=0x5000, pages_cap=1 << 26)), rk.UNSUPPORTED, "too many keys"),
 ])
 def test_accumulate_refusals(L, kw, status, needle):
     a = dict(dict(cache=cache(), chunk=chunk(), q=Q, lse=LSE, w=None, out=W), **kw)

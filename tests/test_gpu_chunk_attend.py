@@ -57,6 +57,21 @@ def test_many_sequences():
     ref.check_attention(c, *attend(c))
 
 
+@pytest.mark.parametrize("news,lens", [([1100], [2000]), ([640, 700], [700, 1500]), ([2200], [2300]), ([300, 3, 400], [900, 1400, 400])])
+def test_tiles_beside_the_chip(news, lens):
+    """From 100 to 290 tiles of 256 rows beside 256 workgroups at a time: cut for one round, for three, or not at all."""
+    c = ref.Case(5, lens, news, 32, 8)
+    ref.check_attention(c, *attend(c))
+
+
+def test_one_workspace_for_all():
+    """A workspace that is used for other calls before and after, of other sizes."""
+    ws = rk.alloc_workspace(rk.OP_CHUNK_ATTEND, ref.Case(6, [10], [1], 2, 1).cache, 1)
+    for lens, news in (([9000], [70]), ([40], [40]), ([9000, 9000], [1, 300]), ([5000], [3])):
+        c = ref.Case(6, lens, news, 4, 1)
+        ref.check_attention(c, *attend(c, ws))
+
+
 def test_large_logits():
     """Maxima that move by hundreds from step to step, and rows that one key dominates."""
     c = ref.Case(5, [1000, 600], [150, 3], 8, 2, scale=6.0)

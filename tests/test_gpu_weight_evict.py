@@ -92,6 +92,25 @@ def test_future_and_garbage_keys():
     assert torch.equal(accumulate(c, lse, None), clean)
 
 
+@pytest.mark.parametrize("tiles,ragged", [(70, 5), (100, 1), (32, 0), (33, 127), (64, 64)])
+def test_tails_of_the_launch(tiles, ragged):
+    """Tiles of 128 keys of eight KV heads beside the 512 workgroups that run at a time: the last ones halved, or not."""
+    n = 128 * tiles - ragged
+    c = ref.Case(37, [n], [40], 8, 8)
+    w_in = torch.rand((1, 8, c.cache.pages_cap * 16), generator=torch.Generator().manual_seed(0)).cuda()
+    lse = ref.attention(c)[1].float()
+    check(c, lse, w_in, accumulate(c, lse, w_in))
+
+
+def test_weights_of_many_sequences():
+    """More sequences than lanes, in the form for many rows and in the one for few."""
+    lens = [1 + (37 * b) % 290 for b in range(150)]
+    for news in ([min(n, 1 + b % 23) for b, n in enumerate(lens)], [1] * 150):
+        c = ref.Case(38, lens, news, 8, 2)
+        lse = ref.attention(c)[1].float()
+        check(c, lse, None, accumulate(c, lse, None))
+
+
 # ---- eviction ----
 
 def random_weights(gen, shape, kind):
@@ -193,6 +212,65 @@ def test_length_beyond_the_cache_counts_as_none():
     kept = torch.empty((2, 1, 20), dtype=torch.int32, device="cuda")
     rk.weight_evict(c.cache, w, 4, 20, dst, None, kept, rk.alloc_workspace(rk.OP_WEIGHT_EVICT, c.cache, 4, 20))
     assert dst.seq_lens.tolist() == [0, 20] and (kept[0] == -1).all() and (dst.k_pool[:8] == 0).all()
+
+
+def test_many_sequences():
+    lens = [1 + (37 * b) % 290 for b in range(150)]
+    c = ref.Case(46, lens, [0] * 150, 2, 1)
+    w = random_weights(torch.Generator().manual_seed(7), (150, 1, c.cache.pages_cap * 16), "plain").cuda()
+    evict_and_check(c, w, 3, 70, 16, False)
+
+
+@pytest.mark.parametrize("lens,keep", [([3000, 500], 300), ([30000, 500], 300)])
+def test_graph_of_accumulation_and_eviction(lens, keep):
+    """Captured once, replayed over other lengths, with eager calls on the same workspace between."""
+    c = ref.Case(47, lens, [40, 3], 4, 2)
+    lse = ref.attention(c)[1].float()
+    w0 = random_weights(torch.Generator().manual_seed(8), (2, 2, c.cache.pages_cap * 16), "plain").cuda()
+    ws = rk.alloc_workspace(rk.OP_WEIGHT_EVICT, c.cache, 16, keep)
+    make = lambda: [torch.empty_like(w0), rk.alloc_cache(2, 4, 2, 128, 16, 24, "cuda", zero=True), torch.zeros((2, 2, 24 * 16), device="cuda"),
+                    torch.zeros((2, 2, keep), dtype=torch.int32, device="cuda")]
+
+    def run(w, dst, w_out, kept):
+        rk.accumulate_weights(c.cache, c.chunk, c.q, lse, w0, w)
+        rk.weight_evict(c.cache, w, 16, keep, dst, w_out, kept, ws)
+
+    a, b = make(), make()
+    a[0].zero_(), b[0].zero_()
+    run(*a)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        run(*a)
+    for cut in (0, 2500, 100, 0):
+        c.cache.seq_lens.copy_(torch.tensor([lens[0] - cut, lens[1] - cut // 10], dtype=torch.int32))
+        for x in (a, b):
+            for t in (x[0], x[1].k_pool, x[1].v_pool, x[2], x[3]):
+                t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        run(*b)
+        for x, y in zip([a[0], a[1].k_pool, a[1].v_pool, a[1].seq_lens, *a[2:]], [b[0], b[1].k_pool, b[1].v_pool, b[1].seq_lens, *b[2:]]):
+            assert torch.equal(x, y)
+    check(c, lse, w0, b[0], fill=0.0)
+
+
+def test_two_streams_at_once():
+    cases = [ref.Case(48 + i, [n], [0], 2, 2) for i, n in enumerate((20000, 3000))]
+    ws = [rk.alloc_workspace(rk.OP_WEIGHT_EVICT, c.cache, 8, 256) for c in cases]
+    w = [random_weights(torch.Generator().manual_seed(9), (1, 2, c.cache.pages_cap * 16), "plain").cuda() for c in cases]
+    kept = [torch.empty((1, 2, 256), dtype=torch.int32, device="cuda") for _ in cases]
+    dst = [rk.alloc_cache(1, 2, 2, 128, 16, 16, "cuda", zero=True) for _ in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for i, c in enumerate(cases):
+            with torch.cuda.stream(streams[i]):
+                rk.weight_evict(c.cache, w[i], 8, 256, dst[i], None, kept[i], ws[i])
+    torch.cuda.synchronize()
+    for i, c in enumerate(cases):
+        for g in range(2):
+            assert np.array_equal(kept[i][0, g].cpu().numpy(), ref.evicted(w[i][0, g].cpu().numpy(), c.lens[0], 8, 256))
 
 
 # ---- together, as a program uses them ----
