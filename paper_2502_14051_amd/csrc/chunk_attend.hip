@@ -205,7 +205,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
   // Keys and values of a step to LDS: every wavefront brings 16 tokens of each, 16 bytes a lane.
   //   keys: [64][16 chunks], chunk x of row r at x ^ r % 16, so that 32 rows at one chunk spread over the banks
   //   values by channel: per page [8 blocks of 16 channels][2 halves of its tokens][16 channels], so that 16 lanes read 256
-  //   bytes in a row; by token: [64][16 chunks], chunk x of row r at x ^ 2 (r % 8)
+  //   bytes in a row; by token: [64][16 chunks], chunk x of row r at x ^ 4 (r % 4)
   constexpr int kLoads = kWaveTok / 4;        // of keys, and of values, a wavefront issues for a step: 1 KiB each
   typedef typename std::conditional<TOK && !FAR, uint32_t, int64_t>::type Offset;  // bytes from the pool's beginning
   const int first_tok = wave * kWaveTok;      // of the step
@@ -275,7 +275,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
     for (int j = 0; j < kLoads; ++j) {
       if (TOK) {
         const int r = first_tok + 4 * j + lane / 16;
-        row_to_lds(c.v_pool, off_v, r, ((lane % 16) ^ 2 * (r % 8)) * 16, vb + j * 1024);
+        row_to_lds(c.v_pool, off_v, r, ((lane % 16) ^ 4 * (lane / 16)) * 16, vb + j * 1024);
       } else {
         to_lds(reinterpret_cast<const char*>(c.v_pool) + off_v, 4096,
                (first_tok % kAttnPage / 4 + j) * 1024 + lane / 32 * 512 + lane % 16 * 32 + lane / 16 % 2 * 16, vb + j * 1024);
@@ -298,18 +298,17 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
     kf = as_bf16x8(*reinterpret_cast<const u32x4*>(s_tiles + (at ^ (uint32_t)(32 * j)) + (decltype(slot)::value * kKeyBytes + u * 8192)));
   };
   // Channels 32 cb + col, tokens 32 u + 16 y + 8 h + 0..7.  By token, lane i of a row of 16 names a piece of token row
-  // 4 z + i / 4 (z: first or second four) and of 16 channels; its chunk 4 cb + a stands at 4 cb ^ 8 z ^ (a ^ 2 (i / 4)), of
-  // which only bit 2 meets a bit of the lane's own: two addresses a lane, the rest is in the instruction.
-  const int vi = lane % 16, va = (2 * (lane / 16 % 2) + vi % 4 / 2) ^ (2 * (vi / 4));
-  const uint32_t value_at = TOK ? (uint32_t)((8 * h + vi / 4) * 256 + vi % 2 * 8 + va * 16) : (uint32_t)(col / 16 * 512 + h * 256 + col % 16 * 16);
-  const uint32_t value_at4 = value_at ^ 64u;
-  const auto read_value = [&](auto slot, int u, int y, int cb, u32x4& vf) {
+  // 4 z + i / 4 (z: first or second four) and of 16 channels; 32 lanes, four token rows, read one after the other, and their
+  // chunks 4 cb + 0..3 stand at 4 (cb ^ i / 4) + 0..3, a place of its own for each.
+  const int vi = lane % 16;
+  const uint32_t value_at = TOK ? (uint32_t)((8 * h + vi / 4) * 256 + vi % 2 * 8 + (4 * (vi / 4) + 2 * (lane / 16 % 2) + vi % 4 / 2) * 16)
+                                : (uint32_t)(col / 16 * 512 + h * 256 + col % 16 * 16);
+  const auto read_value = [&](uint32_t at, auto slot, int u, int y, int cb, u32x4& vf) {
     const int base = (2 + decltype(slot)::value) * kKeyBytes + u * 8192;
     if (TOK) {
       u32x2 w[2];
 #pragma unroll
-      for (int z = 0; z < 2; ++z)
-        w[z] = lds_columns(s_tiles + (cb % 2 ? value_at4 : value_at) + (base + (16 * y + 4 * z) * 256 + ((cb / 2) ^ z) * 128));
+      for (int z = 0; z < 2; ++z) w[z] = lds_columns(s_tiles + (at ^ (uint32_t)(64 * cb)) + (base + (16 * y + 4 * z) * 256));
       vf = (u32x4){w[0].x, w[0].y, w[1].x, w[1].y};
     } else {
       vf = *reinterpret_cast<const u32x4*>(s_tiles + value_at + (base + y * 4096 + cb * 1024));
@@ -431,7 +430,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
       for (int j = 0; j < 8; ++j) {
         fence();
         N = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[j], qf[j], j == 0 ? f32x16{} : N, 0, 0, 0);
-        read_value(slot, u, j / 4, j % 4, vf[j / 4][j % 4]);
+        read_value(value_at, slot, u, j / 4, j % 4, vf[j / 4][j % 4]);
         const float x = exponential(S[2 * j]), y = exponential(S[2 * j + 1]);
         sums[j] = x + y;
         pf[j / 4][j % 4] = pack_bf16x2(x, y);
