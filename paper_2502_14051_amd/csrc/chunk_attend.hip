@@ -33,10 +33,12 @@ constexpr float kLazy = 8.f;              // and followed where it has grown by 
 // 16 bytes per lane straight to LDS: lane l's land 16 l bytes behind the wavefront's `dst`.  From a base that is the same
 // for the wavefront and 32 bits of offset a lane; to_lds_far from any address.  (After loads of the second kind the compiler
 // takes every wait for LDS to be a wait for all of LDS, as it does for accesses through generic pointers.)
+// STREAM: past the caches.
+template <bool STREAM>
 __device__ __forceinline__ void to_lds(const void* base, uint32_t bytes, uint32_t off, unsigned char* dst) {
 #ifdef __HIP_DEVICE_COMPILE__
   __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)bytes, 0x00020000),
-                                           (__attribute__((address_space(3))) void*)dst, 16, (int)off, 0, 0, 0);
+                                           (__attribute__((address_space(3))) void*)dst, 16, (int)off, 0, 0, STREAM ? 2 : 0);
 #endif
 }
 __device__ __forceinline__ void to_lds_far(const void* src, unsigned char* dst) {
@@ -154,7 +156,7 @@ __device__ __forceinline__ bool chunk_place(const CacheView& c, const ChunkAtten
   return true;
 }
 
-template <bool TOK, bool FAR, int WAVES>
+template <bool TOK, bool FAR, int WAVES, bool STREAM>
 __global__ __launch_bounds__(WAVES * kWave) __attribute__((amdgpu_waves_per_eu(2)))
 void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
   constexpr int kWaveTok = kStep / WAVES;  // tokens a wavefront brings
@@ -231,7 +233,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
       const int64_t at = (int64_t)((uint64_t)(uint32_t)__shfl((int)((int64_t)off >> 32), r) << 32 | lo);
       to_lds_far(reinterpret_cast<const char*>(pool) + at + from, dst);
     } else {
-      to_lds(pool, 0xffffffffu, lo + from, dst);
+      to_lds<STREAM>(pool, 0xffffffffu, lo + from, dst);
     }
   };
   // Keys of step `it`, looked up before; looks up the next one.  Returns a bit per token of the step that exists.
@@ -254,7 +256,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
         const int r = first_tok % kAttnPage + 4 * j + lane / 16;
-        to_lds(reinterpret_cast<const char*>(c.k_pool) + off_k, 4096, r * 256 + ((lane % 16) ^ r) * 16, kb + j * 1024);
+        to_lds<STREAM>(reinterpret_cast<const char*>(c.k_pool) + off_k, 4096, r * 256 + ((lane % 16) ^ r) * 16, kb + j * 1024);
       }
       const int left = s.len - it * kStep;
       if (valid == 0xfull && left >= kStep) {
@@ -277,7 +279,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
         const int r = first_tok + 4 * j + lane / 16;
         row_to_lds(c.v_pool, off_v, r, ((lane % 16) ^ 4 * (lane / 16)) * 16, vb + j * 1024);
       } else {
-        to_lds(reinterpret_cast<const char*>(c.v_pool) + off_v, 4096,
+        to_lds<STREAM>(reinterpret_cast<const char*>(c.v_pool) + off_v, 4096,
                (first_tok % kAttnPage / 4 + j) * 1024 + lane / 32 * 512 + lane % 16 * 32 + lane / 16 % 2 * 16, vb + j * 1024);
       }
     }
@@ -563,6 +565,11 @@ ChunkPlan plan_chunk_attend(const CacheView& c, int n_tokens) {
   // which the registers of that form do not suffice)
   p.tile_rows = p.far || (int64_t)n_tokens * c.group > 128ll * c.batch ? 256 : 128;
   p.tile_tokens = p.tile_rows / c.group;
+  // Keys that one tile reads, of caches that the 256 MiB of the last-level cache do not keep until the next call, are read
+  // past the caches: 5 tokens of each of 16 sequences of up to 32768 take 185 us so, 211 without; but 16 tokens behind 4000,
+  // called again at once, 17.8, without 16.5, and where several tiles read the same keys (387 tokens behind 131072, 256 rows
+  // to a tile) 1061, without 946.
+  p.stream = p.tile_rows == 128 && (int64_t)c.batch * c.pages_cap * c.page_size * c.n_kv_heads * kHeadDim * 2 * (int64_t)sizeof(bf16_t) > 256ll << 20;
   p.slots = 256 * (256 / p.tile_rows);
   const int64_t at_least = ((int64_t)n_tokens + p.tile_tokens - 1) / p.tile_tokens * c.n_kv_heads;
   int64_t tiles = (int64_t)n_tokens / p.tile_tokens + c.batch;
@@ -594,11 +601,13 @@ hipError_t launch_chunk_attend(const CacheView& c, const ChunkView& ch, const bf
   const auto launch = [&](auto kernel, int waves) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)plan.workgroups), dim3(waves * kWave), 4 * kKeyBytes, st, c, a);
   };
-  if (plan.far) launch(chunk_attend_kernel<true, true, 8>, 8);
-  else if (plan.tile_rows == 256 && c.v_token_major) launch(chunk_attend_kernel<true, false, 8>, 8);
-  else if (plan.tile_rows == 256) launch(chunk_attend_kernel<false, false, 8>, 8);
-  else if (c.v_token_major) launch(chunk_attend_kernel<true, false, 4>, 4);
-  else launch(chunk_attend_kernel<false, false, 4>, 4);
+  if (plan.far) launch(chunk_attend_kernel<true, true, 8, false>, 8);
+  else if (plan.tile_rows == 256 && c.v_token_major) launch(chunk_attend_kernel<true, false, 8, false>, 8);
+  else if (plan.tile_rows == 256) launch(chunk_attend_kernel<false, false, 8, false>, 8);
+  else if (c.v_token_major && plan.stream) launch(chunk_attend_kernel<true, false, 4, true>, 4);
+  else if (c.v_token_major) launch(chunk_attend_kernel<true, false, 4, false>, 4);
+  else if (plan.stream) launch(chunk_attend_kernel<false, false, 4, true>, 4);
+  else launch(chunk_attend_kernel<false, false, 4, false>, 4);
   if (plan.cuts) {
     hipLaunchKernelGGL(chunk_merge_kernel, dim3(plan.most, kMergeSlices), dim3(kMergeWaves * kWave), 0, st, c, a, plan.tile_rows);
   }

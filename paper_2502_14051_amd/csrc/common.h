@@ -402,6 +402,7 @@ hipError_t launch_append_chunk(const CacheView& c, const ChunkView& ch, const Ro
 struct ChunkPlan {
   int tile_rows, tile_tokens;
   bool far;         // a token-major pool's rows need 64 bits of offset
+  bool stream;      // keys and values are read past the caches
   int slots, most;  // workgroups the chip holds at a time; parts that keys may be divided into, of all tiles together
   bool cuts;        // keys may be divided
   int64_t workgroups;

@@ -64,6 +64,13 @@ def test_tiles_beside_the_chip(news, lens):
     ref.check_attention(c, *attend(c))
 
 
+@pytest.mark.parametrize("ps,token_major", [(16, False), (4, True)])
+def test_caches_beyond_the_last_level(ps, token_major):
+    """More room than 256 MiB and few rows: the form that reads past the caches."""
+    c = ref.Case(7, [700, 5000, 1], [3, 20, 1], 8, 2, ps, token_major, spare_pages=100000 // ps)
+    ref.check_attention(c, *attend(c))
+
+
 def test_one_workspace_for_all():
     """A workspace that is used for other calls before and after, of other sizes."""
     ws = rk.alloc_workspace(rk.OP_CHUNK_ATTEND, ref.Case(6, [10], [1], 2, 1).cache, 1)
