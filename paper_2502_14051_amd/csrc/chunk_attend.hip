@@ -13,6 +13,16 @@
 // product leaves a lane the keys of A's rows 8a + 4h + r; with the rows of K read in an order that swaps bits 2 and 3,
 // these are keys 16x + 8h + 0..7, which packed to bf16 are the second product's operand as they stand.  P is rounded to
 // bf16 there (relative 2^-8 at most each, the sum l takes the unrounded values); everything else is fp32.
+//
+// What bounds it.  Many rows: the matrix cores and, beside them, the vector instructions of the exponentials, at the clock
+// that the chip's power leaves (2.0 GHz).  2048 tokens of 32 heads behind 32768, 8 KV heads, take 1.04 to 1.09 ms, 1.05 to
+// 1.09 PFLOP/s, the matrix cores busy 52 % of the cycles; without loads and LDS reads the same instructions ran at 1.30, a
+// library's product of 8192^3 runs at 1.40.  Few rows: HBM, 6.2 TB/s for 5 tokens of each of 16 sequences of up to 32768.
+// Why 32 rows to a wavefront and two wavefronts to a SIMD: one stands at its products while the other forms exponentials.
+// 64 rows, one wavefront to a SIMD, would read keys and values half as often, but its sums then travel between the two
+// register files every step: 0.65 PFLOP/s; the two wavefronts alternating by barriers 0.62 to 0.87; products and
+// exponentials of one unit one after the other 0.92; with the next unit's operands requested ahead 0.97; exponentials
+// beside the products, fenced so that they stay there, 1.05; and with a raised priority while they do, 1.09.
 #include <type_traits>
 
 #include "attend_core.h"
