@@ -486,39 +486,42 @@ class Rope:
     scale: float = 1.0
 
     def struct(self) -> RopeStruct:
-        _tensor("inv_freq", self.inv_freq, "float64", (None,))
+        _tensor("inv_freq", self.inv_freq, "float64", self.inv_freq.shape[:1] or (0,))
         return RopeStruct(2 * int(self.inv_freq.shape[0]), int(self.interleaved), _ptr(self.inv_freq), self.scale)
 
 
 _dtypes = {}
 
 
-def _current_device():
-    import torch  # (where a tensor lies on a GPU, torch.cuda.current_device has nothing left to initialise)
-    return torch._C._cuda_getDevice()
-
-
 def _tensor(name, t, dtype, shape, rows=False):
-    """What a pointer cannot say: type, shape (None: any) and layout, contiguous or, with `rows`, tokens at any stride."""
+    """What a pointer cannot say: type, shape and layout, contiguous or, with `rows`, tokens at any stride."""
     want = _dtypes.get(dtype)
     if want is None:
         import torch
         want = _dtypes[dtype] = getattr(torch, dtype)
     have = t.shape
-    ok = t.dtype is want and (have == shape or len(have) == len(shape) and all(w is None or w == h for w, h in zip(shape, have)))
-    if not ok:
+    if t.dtype is not want or have != shape:
         raise RocketKVError(INVALID_ARG, f"{name}: need {dtype} {tuple(shape)}, got {t.dtype} {tuple(have)}")
-    device = t.get_device()
-    if device < 0 or device != _current_device():
-        raise RocketKVError(INVALID_ARG, f"{name}: on {t.device}, not on the current GPU")
     if not t.is_contiguous() and not (rows and t.stride()[1:] == (have[2], 1)):
         raise RocketKVError(INVALID_ARG, f"{name}: inner dimensions must be contiguous")
 
 
-def _row_stride(t):
-    """Elements between tokens (a single token may have any)."""
-    n, heads, channels = t.shape
-    return t.stride(0) if n > 1 else heads * channels
+def _here(**tensors):
+    """All of them (but for None) on the current GPU."""
+    here = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        device = t.get_device()
+        if here is None and device >= 0:
+            import torch  # (with a tensor on a GPU, torch.cuda.current_device has nothing left to initialise)
+            here = torch._C._cuda_getDevice()
+        if device != here:
+            raise RocketKVError(INVALID_ARG, f"{name}: on {t.device}, not on the current GPU")
+
+
+def _here_with(cache, **tensors):
+    _here(k_pool=cache.k_pool, v_pool=cache.v_pool, seq_lens=cache.seq_lens, block_table=cache.block_table, **tensors)
 
 
 def rope_frequencies(rot_dim: int, theta: float, kind: int = ROPE_PLAIN, factor: float = 1.0, low: float = 1.0,
@@ -534,37 +537,42 @@ def rope_frequencies(rot_dim: int, theta: float, kind: int = ROPE_PLAIN, factor:
 
 def rope(rope: Rope, positions, x, y, stream=None):
     """x, y: bf16 [tokens][heads][128], tokens at any stride; positions: int32 [tokens].  y may be x."""
-    _tensor("x", x, "bfloat16", (None, None, 128), rows=True)
-    n, heads, _ = x.shape
+    _tensor("x", x, "bfloat16", x.shape[:2] + (128,), rows=True)
+    n, heads, width = x.shape
     _tensor("y", y, "bfloat16", (n, heads, 128), rows=True)
     _tensor("positions", positions, "int32", (n,))
+    r = rope.struct()
+    _here(x=x, y=y, positions=positions, inv_freq=rope.inv_freq)
     if n == 0:
         return
-    r = rope.struct()
-    _check(lib().rocketkv_rope(C.byref(r), _ptr(positions), n, heads, _ptr(x), _row_stride(x), _ptr(y), _row_stride(y),
-                               _stream(stream)))
+    width *= heads  # (a single token's stride may be anything)
+    _check(lib().rocketkv_rope(C.byref(r), _ptr(positions), n, heads, _ptr(x), x.stride(0) if n > 1 else width, _ptr(y),
+                               y.stride(0) if n > 1 else width, _stream(stream)))
 
 
 def append_chunk(cache: Cache, chunk: Chunk, k_new, v_new, kmax, kmin, workspace, rope: Optional[Rope] = None,
                  positions=None, q=None, q_out=None, stream=None):
     """k_new, v_new: bf16 [n_tokens][n_kv_heads][128], q: bf16 [n_tokens][n_q_heads][128], tokens at any stride."""
     n = chunk.n_tokens
-    for name, t, heads in (("k_new", k_new, cache.n_kv_heads), ("v_new", v_new, cache.n_kv_heads), ("q", q, cache.n_q_heads)):
-        if t is not None:
-            _tensor(name, t, "bfloat16", (n, heads, 128), rows=True)
+    _tensor("k_new", k_new, "bfloat16", (n, cache.n_kv_heads, 128), rows=True)
+    _tensor("v_new", v_new, "bfloat16", (n, cache.n_kv_heads, 128), rows=True)
+    if q is not None:
+        _tensor("q", q, "bfloat16", (n, cache.n_q_heads, 128), rows=True)
     if q_out is not None:
         _tensor("q_out", q_out, "bfloat16", (n, cache.n_q_heads, 128))
     if positions is not None:
         _tensor("positions", positions, "int32", (n,))
     _summaries(cache, kmax, kmin)
+    st, ch, r = cache.struct(), chunk.struct(cache), rope.struct() if rope is not None else None
+    _here_with(cache, k_new=k_new, v_new=v_new, q=q, q_out=q_out, positions=positions, kmax=kmax, kmin=kmin,
+               starts=chunk.starts, inv_freq=rope.inv_freq if rope is not None else None, workspace=workspace)
     if n == 0:
         return
-    st, ch, r = cache.struct(), chunk.struct(cache), rope.struct() if rope is not None else None
-    stride = lambda t: 0 if t is None else _row_stride(t)
+    stride = lambda t, heads: t.stride(0) if n > 1 and t is not None else heads * 128
     _check(lib().rocketkv_append_chunk(C.byref(st), C.byref(ch), C.byref(r) if r is not None else None, _ptr(positions),
-                                       _ptr(q), stride(q), _ptr(q_out), _ptr(k_new), stride(k_new), _ptr(v_new),
-                                       stride(v_new), _ptr(kmax), _ptr(kmin), _ptr(workspace), workspace.numel(),
-                                       _stream(stream)))
+                                       _ptr(q), stride(q, cache.n_q_heads), _ptr(q_out), _ptr(k_new),
+                                       stride(k_new, cache.n_kv_heads), _ptr(v_new), stride(v_new, cache.n_kv_heads),
+                                       _ptr(kmax), _ptr(kmin), _ptr(workspace), workspace.numel(), _stream(stream)))
 
 
 def _summaries(cache, kmax, kmin):
@@ -580,9 +588,10 @@ def chunk_attend(cache: Cache, chunk: Chunk, q, out, out_lse, workspace, stream=
     _tensor("out", out, "bfloat16", (n, cache.n_q_heads, 128))
     if out_lse is not None:
         _tensor("out_lse", out_lse, "float32", (n, cache.n_q_heads))
+    st, ch = cache.struct(), chunk.struct(cache)
+    _here_with(cache, q=q, out=out, out_lse=out_lse, starts=chunk.starts, workspace=workspace)
     if n == 0:
         return
-    st, ch = cache.struct(), chunk.struct(cache)
     _check(lib().rocketkv_chunk_attend(C.byref(st), C.byref(ch), _ptr(q), _ptr(out), _ptr(out_lse), _ptr(workspace),
                                        workspace.numel(), _stream(stream)))
 
@@ -608,6 +617,7 @@ def accumulate_weights(cache: Cache, chunk: Chunk, q, lse, weights_in, weights_o
         _weights("weights_in", weights_in, cache)
     _weights("weights_out", weights_out, cache)
     st, ch = cache.struct(), chunk.struct(cache)
+    _here_with(cache, q=q, lse=lse, weights_in=weights_in, weights_out=weights_out, starts=chunk.starts)
     _check(lib().rocketkv_accumulate_weights(C.byref(st), C.byref(ch), _ptr(q), _ptr(lse), _ptr(weights_in),
                                              _ptr(weights_out), _stream(stream)))
 
@@ -620,6 +630,8 @@ def weight_evict(src: Cache, weights, n_recent: int, keep_budget: int, dst: Cach
     if kept_idx is not None:
         _tensor("kept_idx", kept_idx, "int32", (src.batch, src.n_kv_heads, keep_budget))
     s, d = src.struct(), dst.struct()
+    _here_with(src, weights=weights, dst_weights=dst_weights, kept_idx=kept_idx, workspace=workspace)
+    _here_with(dst)
     _check(lib().rocketkv_weight_evict(C.byref(s), _ptr(weights), n_recent, keep_budget, C.byref(d), _ptr(dst_weights),
                                        _ptr(kept_idx), _ptr(workspace), workspace.numel(), _stream(stream)))
 

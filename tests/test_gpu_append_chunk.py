@@ -1,4 +1,6 @@
 """Rotary positions, and new tokens into the cache."""
+import dataclasses
+
 import pytest
 import torch
 
@@ -214,6 +216,12 @@ def test_tensors_of_another_kind_are_refused():
         rk.append_chunk(c.cache, rk.Chunk(c.chunk.starts[:2], c.rows), k, v, kmax, kmin, ws)
     with pytest.raises(rk.RocketKVError):
         rk.append_chunk(c.cache, c.chunk, k, v, kmax, kmin, ws[:1024])
+    for name in ("k_pool", "v_pool", "seq_lens", "block_table"):  # a cache that lies elsewhere, in part or as a whole
+        other = dataclasses.replace(c.cache, **{name: getattr(c.cache, name).cpu()})
+        for call in (lambda: rk.append_chunk(other, c.chunk, k, v, kmax, kmin, ws),
+                     lambda: rk.weight_evict(c.cache, rk.alloc_weights(c.cache), 1, 2, other, None, None, ws)):
+            with pytest.raises(rk.RocketKVError, match=name + ": on cpu"):
+                call()
 
 
 def test_no_tokens_at_all():
