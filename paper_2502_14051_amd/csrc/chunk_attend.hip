@@ -119,8 +119,14 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const CacheView& c, const ChunkVie
   return s;
 }
 
-// Every wavefront derives the same division from the lengths.
-__device__ __forceinline__ int chunk_size_for(const CacheView& c, const ChunkAttendArgs& a) {
+// Every wavefront derives the same division from the lengths.  `own`: sequence `lane` of the first 64, which most batches
+// are all of: looked up once, as each look is a round trip that nothing hides.
+__device__ __forceinline__ ChunkSeq chunk_seq_of_lane(const CacheView& c, const ChunkView& ch) {
+  const int lane = threadIdx.x % kWave;
+  if (lane < c.batch) return chunk_seq(c, ch, lane);
+  return {0, 0, 0};
+}
+__device__ __forceinline__ int chunk_size_for(const CacheView& c, const ChunkAttendArgs& a, const ChunkSeq& own) {
   const int lane = threadIdx.x % kWave;
   if (!a.partial) return kChunkWhole;
   const auto total = [](int x) { return __builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)x), kWave - 1); };
@@ -129,7 +135,7 @@ __device__ __forceinline__ int chunk_size_for(const CacheView& c, const ChunkAtt
     for (int b0 = 0; b0 < c.batch; b0 += kWave) {
       int t = 0, steps = 0;
       if (b0 + lane < c.batch) {
-        const ChunkSeq s = chunk_seq(c, a.ch, b0 + lane);
+        const ChunkSeq s = b0 == 0 ? own : chunk_seq(c, a.ch, b0 + lane);
         t = chunk_ceil(s.n, a.tile_tokens);
         steps = t ? chunk_ceil(s.len, kStep) : 0;
       }
@@ -149,14 +155,16 @@ __device__ __forceinline__ int chunk_size_for(const CacheView& c, const ChunkAtt
   });
 }
 
-__device__ __forceinline__ bool chunk_place(const CacheView& c, const ChunkAttendArgs& a, int size, int at, ChunkPlace& p) {
+__device__ __forceinline__ bool chunk_place(const CacheView& c, const ChunkAttendArgs& a, const ChunkSeq& own, int size, int at,
+                                            ChunkPlace& p, ChunkSeq& s) {
   int idx;
   if (!locate_tile(c.batch, at, [&](int i) {
-        const ChunkSeq s = chunk_seq(c, a.ch, i);
+        const ChunkSeq s = i < kWave ? own : chunk_seq(c, a.ch, i);
         return chunk_ceil(s.n, a.tile_tokens) * chunk_parts(chunk_ceil(s.len, kStep), size);
       }, p.b, idx))
     return false;
-  const ChunkSeq s = chunk_seq(c, a.ch, p.b);
+  if (p.b < kWave) s = {__builtin_amdgcn_readlane(own.row, p.b), __builtin_amdgcn_readlane(own.n, p.b), __builtin_amdgcn_readlane(own.len, p.b)};
+  else s = chunk_seq(c, a.ch, p.b);
   p.parts = chunk_parts(chunk_ceil(s.len, kStep), size);
   // the tiles of one part side by side, as they read the same keys; those that see most first
   p.next = chunk_ceil(s.n, a.tile_tokens);
@@ -176,14 +184,15 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
   const int col = lane % 32, h = lane / 32;
   const int g = blockIdx.x % c.n_kv_heads, at = blockIdx.x / c.n_kv_heads;
   ChunkPlace pl;
-  const bool any = chunk_place(c, a, chunk_size_for(c, a), at, pl);
+  ChunkSeq s;
+  const ChunkSeq own = chunk_seq_of_lane(c, a.ch);
+  const bool any = chunk_place(c, a, own, chunk_size_for(c, a, own), at, pl, s);
   const bool holds = a.partial && (int)blockIdx.x < a.most;  // a place for a part's rows
   if (!any) {
     if (holds && threadIdx.x == 0) a.part_place[blockIdx.x] = make_int4(0, 0, 1, 0);
     return;
   }
   if (pl.parts > 1 && !holds) return;  // (`starts` that overlap)
-  const ChunkSeq s = chunk_seq(c, a.ch, pl.b);
   const int G = c.group, ps = c.page_size;
   const int t0 = pl.tile * a.tile_tokens, nt = min(a.tile_tokens, s.n - t0);
   const int rows = nt * G;
