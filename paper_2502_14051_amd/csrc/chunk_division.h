@@ -5,6 +5,8 @@
 // at a time.  Where the tiles alone would leave compute units idle, the keys of every tile are cut as well and the parts
 // are merged by a second launch.  A part is not free: its rows' sums go to memory and come back, and it begins with steps
 // that overlap nothing; together what kChunkPartSteps steps of its work take.
+// (For a prompt alone, whose last tile sees twice the mean, parts of the long tiles only were no gain either: 2048 tokens
+// 80 us so, 68 whole.)
 #pragma once
 #include <stdint.h>
 
@@ -42,7 +44,8 @@ RKV_HD constexpr int chunk_rounds(int64_t tiles, int slots) { return 2 * tiles >
 // unless the tiles do; `count(size)`: workgroups at that size.
 template <class Count>
 RKV_HD inline int chunk_part_size(const ChunkLoad& load, int slots, int most, const Count& count) {
-  if (load.tiles >= most || load.longest <= kChunkLeastSteps) return kChunkWhole;
+  // (a part of the least size already costs what the whole of so short a tile does)
+  if (load.tiles >= most || load.longest <= kChunkLeastSteps + kChunkPartSteps) return kChunkWhole;
   int best = kChunkWhole;
   int64_t cost = (int64_t)chunk_ceil(load.tiles, slots) * load.longest;
   for (int limit = slots; limit <= most; limit += slots) {
