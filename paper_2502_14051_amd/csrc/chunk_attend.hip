@@ -601,7 +601,9 @@ ChunkPlan plan_chunk_attend(const CacheView& c, int n_tokens) {
   tiles *= c.n_kv_heads;
   const int rounds = chunk_rounds(at_least, p.slots);
   p.most = p.slots * rounds;
-  p.cuts = at_least < p.most;
+  // Where no sequence can be long enough to be cut, neither the merge nor the workgroups of parts are launched: a prompt of
+  // 300 tokens 14.9 us, 17.2 with them.
+  p.cuts = at_least < p.most && (int64_t)c.pages_cap * c.page_size > kChunkShort * kStep;
   p.workgroups = p.cuts && tiles < p.most ? p.most : tiles;
   // (for any number of tokens, so that what serves many serves few)
   p.total_bytes = n_tokens ? (size_t)ROCKETKV_WS_HEADER_BYTES + (size_t)256 * kChunkRounds * (256 * (kHeadDim + 2) * sizeof(float) + 2 * sizeof(int4)) : 0;

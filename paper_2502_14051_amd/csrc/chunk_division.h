@@ -20,6 +20,7 @@ namespace rkv {
 
 constexpr int kChunkPartSteps = 8;
 constexpr int kChunkLeastSteps = 4;     // no part is smaller
+constexpr int kChunkShort = kChunkLeastSteps + kChunkPartSteps;  // a part of the least size costs what so short a tile does
 constexpr int kChunkRounds = 3;         // parts for up to so many rounds of workgroups over the chip, see chunk_rounds
 constexpr int kChunkWhole = 1 << 30;    // nothing is cut
 
@@ -44,8 +45,7 @@ RKV_HD constexpr int chunk_rounds(int64_t tiles, int slots) { return 2 * tiles >
 // unless the tiles do; `count(size)`: workgroups at that size.
 template <class Count>
 RKV_HD inline int chunk_part_size(const ChunkLoad& load, int slots, int most, const Count& count) {
-  // (a part of the least size already costs what the whole of so short a tile does)
-  if (load.tiles >= most || load.longest <= kChunkLeastSteps + kChunkPartSteps) return kChunkWhole;
+  if (load.tiles >= most || load.longest <= kChunkShort) return kChunkWhole;
   int best = kChunkWhole;
   int64_t cost = (int64_t)chunk_ceil(load.tiles, slots) * load.longest;
   for (int limit = slots; limit <= most; limit += slots) {

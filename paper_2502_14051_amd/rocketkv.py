@@ -209,11 +209,12 @@ class Cache:
     v_layout: int = V_CHANNEL_MAJOR
 
     def struct(self) -> CacheStruct:
-        assert self.k_pool.stride()[:2] == self.v_pool.stride()[:2], "K and V pools must share strides"
-        return CacheStruct(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim,
-                           self.page_size, self.pages_cap, int(self.k_pool.shape[0]),
-                           int(self.k_pool.stride(0)), int(self.k_pool.stride(1)), _ptr(self.seq_lens),
-                           _ptr(self.block_table), _ptr(self.k_pool), _ptr(self.v_pool), self.v_layout)
+        k_pool, table = self.k_pool, self.block_table
+        strides = k_pool.stride()
+        assert strides[:2] == self.v_pool.stride()[:2], "K and V pools must share strides"
+        return CacheStruct(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_size, self.pages_cap,
+                           k_pool.shape[0], strides[0], strides[1], self.seq_lens.data_ptr(),
+                           None if table is None else table.data_ptr(), k_pool.data_ptr(), self.v_pool.data_ptr(), self.v_layout)
 
     @property
     def units(self) -> int:
