@@ -618,9 +618,10 @@ hipError_t launch_chunk_attend(const CacheView& c, const ChunkView& ch, const bf
   a.q = q;
   a.out = out;
   a.out_lse = out_lse;
+  const int64_t part_rows = (int64_t)plan.most * plan.tile_rows;
   a.partial = plan.cuts ? reinterpret_cast<float*>(static_cast<char*>(ws) + ROCKETKV_WS_HEADER_BYTES) : nullptr;
-  a.part_stats = reinterpret_cast<float2*>(a.partial + (int64_t)plan.most * plan.tile_rows * kHeadDim);
-  a.part_place = reinterpret_cast<int4*>(a.part_stats + (int64_t)plan.most * plan.tile_rows);
+  a.part_stats = plan.cuts ? reinterpret_cast<float2*>(a.partial + part_rows * kHeadDim) : nullptr;
+  a.part_place = plan.cuts ? reinterpret_cast<int4*>(a.part_stats + part_rows) : nullptr;
   a.tile_tokens = plan.tile_tokens;
   a.slots = plan.slots;
   a.most = plan.most;
