@@ -213,7 +213,7 @@ class Cache:
         strides = k_pool.stride()
         assert strides[:2] == self.v_pool.stride()[:2], "K and V pools must share strides"
         return CacheStruct(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_size, self.pages_cap,
-                           k_pool.shape[0], strides[0], strides[1], self.seq_lens.data_ptr(),
+                           k_pool.shape[0], strides[0], strides[1], _ptr(self.seq_lens),
                            None if table is None else table.data_ptr(), k_pool.data_ptr(), self.v_pool.data_ptr(), self.v_layout)
 
     @property
