@@ -512,7 +512,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
     return;
   }
   const int64_t row = packed_row((int)use_late((uint32_t)r));
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (a sum that is NaN stays one, here and below: only 0 is no key at all)
   bf16_t* o = a.out + row * kHeadDim + 4 * h;
 #pragma unroll
   for (int cb = 0; cb < 4; ++cb)
@@ -520,7 +520,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
     for (int i = 0; i < 16; i += 4)
       *reinterpret_cast<u32x2*>(o + 32 * cb + 2 * i) =
           (u32x2){pack_bf16x2(O[cb][i] * inv, O[cb][i + 1] * inv), pack_bf16x2(O[cb][i + 2] * inv, O[cb][i + 3] * inv)};
-  if (a.out_lse && h == 0) a.out_lse[row] = sum > 0.f ? (m + __log2f(sum)) * kLn2 : -INFINITY;
+  if (a.out_lse && h == 0) a.out_lse[row] = sum == 0.f ? -INFINITY : (m + __log2f(sum)) * kLn2;
 }
 
 constexpr int kMergeWaves = 8, kMergeSlices = 2;  // wavefronts to a workgroup, workgroups to a part
@@ -569,9 +569,9 @@ __global__ __launch_bounds__(kMergeWaves * kWave) void chunk_merge_kernel(CacheV
     for (int d = 1; d < kWave; d *= 2) l += __shfl_xor(l, d);
     const int t = r / G;
     const int64_t row = (int64_t)(place.x + t) * c.n_q_heads + (int64_t)g * G + r - t * G;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
     *reinterpret_cast<uint32_t*>(a.out + row * kHeadDim + 2 * lane) = pack_bf16x2(x * inv, y * inv);
-    if (a.out_lse && lane == 0) a.out_lse[row] = l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
+    if (a.out_lse && lane == 0) a.out_lse[row] = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
   }
 }
 
