@@ -450,8 +450,10 @@ int32_t rocketkv_accumulate_weights(const rocketkv_cache_t* cache, const rocketk
  * Eviction by accumulated weight.  Per (sequence, KV head) of S = src->seq_lens[b] tokens: all are kept if
  * S <= keep_budget; otherwise the last n_recent tokens and, of the others, the keep_budget - n_recent with the largest
  * weight (ties: lower position; NaN counts as larger than every number).  K, V and weights of the kept tokens go to
- * `dst`, in ascending position, and dst->seq_lens[b] = min(S, keep_budget).  src is left as it is.  Of a kept token whose
- * page is absent nothing moves but its weight.  A sequence longer than src counts as empty.
+ * `dst`, in ascending position, and dst->seq_lens[b] = min(S, keep_budget).  src is left as it is.  A kept token whose page
+ * is absent in src takes a place in dst like any other, with zeros for key and value (and its weight): from there on it is
+ * a token, where attention over src skipped it.  A token of an absent page of dst goes nowhere.  A sequence longer than src
+ * counts as empty.  A channel-major dst gets whole tiles, zeros behind the last token.
  * weights: fp32 [batch][n_kv_heads][src->pages_cap * src->page_size], 16-byte aligned.
  * dst: a cache with pools and lengths of its own, the same head counts, room for keep_budget tokens, any page size and
  *      V layout (channel-major: page_size 16, for src as well).

@@ -335,6 +335,7 @@ __global__ __launch_bounds__(kEvictT) void evict_select_kernel(CacheView c, Evic
 }
 
 // 64 kept tokens to their places.  Key rows move as 256-byte rows, and so do value rows between token-major caches.
+// A kept token whose page is absent counts in the destination like any other: its place is filled with zeros.
 // A channel-major source tile is read whole by a wavefront, 16 bytes a lane, once for all of its kept tokens (the lines
 // of its 128 channels are touched by any one of them), and the kept columns go to LDS in the order the destination wants.
 template <bool SRC_TOK, bool DST_TOK>
@@ -375,13 +376,13 @@ __global__ __launch_bounds__(256) void evict_move_kernel(CacheView src, CacheVie
   const auto store_keys = [&]() {
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if (to[u] >= 0 && (from[u] >= 0 || !DST_TOK)) *reinterpret_cast<uint4*>(dst.k_pool + to[u]) = kv[u];
+      if (to[u] >= 0) *reinterpret_cast<uint4*>(dst.k_pool + to[u]) = kv[u];
   };
   if (SRC_TOK && DST_TOK) {
     store_keys();
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if (to[u] >= 0 && from[u] >= 0) *reinterpret_cast<uint4*>(dst.v_pool + to[u]) = vv[u];
+      if (to[u] >= 0) *reinterpret_cast<uint4*>(dst.v_pool + to[u]) = vv[u];
     return;
   }
   if (SRC_TOK) {
@@ -427,7 +428,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(CacheView src, CacheVie
   if (DST_TOK) {
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if (to[u] >= 0 && from[u] >= 0)
+      if (to[u] >= 0)
         *reinterpret_cast<uint4*>(dst.v_pool + to[u]) = *reinterpret_cast<const uint4*>(s_v + (row + 16 * u) * kRowPitch + piece * 8);
   } else {
 #pragma unroll
