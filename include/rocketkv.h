@@ -441,7 +441,8 @@ int32_t rocketkv_chunk_attend(const rocketkv_cache_t* cache, const rocketkv_chun
  * for j < seq_lens[b]; later entries are left as they were.  weights: fp32 [batch][n_kv_heads][pages_cap * page_size].
  * weights_in NULL counts as zeros and may be weights_out itself.  q and lse: as given to and left by
  * rocketkv_chunk_attend (or, with a chunk of one token per sequence, by rocketkv_dense_decode); a row whose lse is -inf
- * adds nothing, nor does a token in an absent page receive any.
+ * adds nothing whatever its query holds, nor does a token in an absent page receive any.  A row whose lse is NaN makes the
+ * weights of the tokens that it sees NaN, and no others.
  */
 int32_t rocketkv_accumulate_weights(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const void* q,
                                     const float* lse, const float* weights_in, float* weights_out, void* stream);

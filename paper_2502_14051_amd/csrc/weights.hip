@@ -61,6 +61,67 @@ __device__ __forceinline__ int weight_len(const CacheView& c, int b) {
   return n < 0 ? 0 : min(n, c.pages_cap * c.page_size);
 }
 
+// What a sequence's rows from `r0` on bring to the 32 keys of a wavefront, straight from memory, 32 rows at a time; the
+// lane's key is `age` tokens behind the chunk's first (negative: before it), kf its channels 16 j + 8 h ..  The two halves'
+// sums are to be added up.
+// A row that has no log sum-exp, or does not see the key, adds exp2 of -inf.  That is NaN where its logit is NaN or +inf (or,
+// in the loop of many rows, its log sum-exp is NaN).  No loop looks for it: it is the sum that shows, and is formed again
+// CAREFULly, with such rows left out whatever their logit is (done so always, a step of 16 sequences took 30.5 us, 29.2 so).
+template <bool CAREFUL>
+__device__ __forceinline__ float sum_of_rows(const CacheView& c, const WeightArgs& a, const u32x4 (&kf)[8], float* s_lse, int g,
+                                             int row0, int rows, int r0, int age, int col, int h) {
+  const int G = c.group;
+  const float sc = kLog2e * 0.08838834764831845f;  // log2(e) / sqrt(128)
+  float sum = 0.f;
+  for (; r0 < rows; r0 += 32) {
+    const int r = min(r0 + col, rows - 1), t = r / G;
+    const int64_t row = (int64_t)(row0 + t) * c.n_q_heads + (int64_t)g * G + (r - t * G);
+    u32x4 qf[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) qf[j] = ld_plain<u32x4>(a.q + row * kHeadDim + h * 8 + j * 16);
+    const float l = a.lse[row];
+    const bool adds = l != -INFINITY && r0 + col < rows;
+    if (h == 0) s_lse[col] = adds ? l * kLog2e : CAREFUL ? -INFINITY : INFINITY;
+    f32x16 S;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qf[j]), as_bf16x8(kf[j]), j == 0 ? f32x16{} : S, 0, 0, 0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (written and read by this wavefront alone)
+    const int first = max(0, age) * G - r0 - 4 * h;     // row of the block that sees the key first
+    float part = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const f32x4 rl = *reinterpret_cast<const f32x4*>(&s_lse[2 * i + 4 * h]);
+      float e[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        e[x] = 2 * i + x < first || (CAREFUL && rl[x] == -INFINITY) ? 0.f : fast_exp2(fmaf(S[i + x], sc, -rl[x]));
+      part += (e[0] + e[1]) + (e[2] + e[3]);
+    }
+    sum += part;
+    asm volatile("" ::: "memory");
+  }
+  return sum;
+}
+
+// The weights of those of 32 keys whose sum so far is NaN.  (Everything looked up anew, so that nothing is held for this
+// through the loop in front of it.)
+__device__ __forceinline__ void careful_weights(const CacheView& c, const WeightArgs& a, float* s_lse, int b, int g, int key0,
+                                                float sum, int col, int h) {
+  const int len = weight_len(c, b), key = key0 + col;
+  const int64_t pp = key < len ? phys_page(c, b, key / c.page_size) : -1;
+  const bf16_t* k = c.k_pool + (pp >= 0 ? pp * c.stride_page + (int64_t)g * c.stride_head + (int64_t)(key % c.page_size) * kHeadDim : 0) + h * 8;
+  u32x4 kf[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) kf[j] = ld_plain<u32x4>(k + j * 16);
+  const int n = chunk_rows(a.ch, b), old = len - n;
+  const float careful = sum_of_rows<true>(c, a, kf, s_lse, g, chunk_first(a.ch, b), n * c.group, 0, key - old, col, h);
+  const SwapPair sw = swap_rows32(__float_as_uint(careful));
+  if (h != 0 || pp < 0 || sum == sum) return;
+  const int64_t at = ((int64_t)b * c.n_kv_heads + g) * ((int64_t)c.pages_cap * c.page_size) + key;
+  a.w_out[at] = (a.w_in && key < old ? a.w_in[at] : 0.f) + (__uint_as_float(sw.a) + __uint_as_float(sw.b));
+}
+
 // A wavefront holds NK blocks of 32 keys.  Two take the first 64 rows of a step, two the same keys and the other 64: a
 // workgroup is done with 128 keys in half the time that four wavefronts of keys of their own take for 256, and the last
 // ones of a launch leave less of the chip idle.  A unit is 32 rows; its exponentials stand beside the next unit's
@@ -110,11 +171,14 @@ __device__ __forceinline__ void weights_of_keys(const CacheView& c, const Weight
       const uint32_t x = (uint32_t)(skip + r), t = x * per_G >> 16;
       return t * (uint32_t)c.n_q_heads + (x - t * (uint32_t)G);
     };
+    // (added up here each time, rather than in eight registers of their own through the loop)
+    int mine_at = wave * (kRowStep / kWeightWaves) * 256;
+    asm volatile("" : "+s"(mine_at));
 #pragma unroll
     for (int j = 0; j < kRowStep / kWeightWaves / 4; ++j) {
       const int r = wave * (kRowStep / kWeightWaves) + 4 * j + lane / 16;
       to_lds(a.q + first * kHeadDim, place(min(r, left - 1)) * 256u + ((lane % 16) ^ r % 16) * 16,
-             s_q[decltype(to)::value] + (wave * (kRowStep / kWeightWaves) + 4 * j) * 256);
+             s_q[decltype(to)::value] + mine_at + 4 * j * 256);
     }
     const int r = wave * kWave + lane;
     lse = r < kRowStep && r < left ? a.lse[first + place(r)] : -INFINITY;
@@ -216,15 +280,23 @@ __device__ __forceinline__ void weights_of_keys(const CacheView& c, const Weight
     if (own_rows != 0 && here < 32) s_sum[(kw * NK + x) * 32 + here] = sum[x];
   }
   __syncthreads();
-  if (own_rows != 0 || here >= 32) return;
+  if (own_rows != 0) return;
+  bool again = false;
 #pragma unroll
   for (int x = 0; x < NK; ++x) {
-    const int at_key = (kw * NK + x) * 32 + here, key = key0 + at_key;
-    if (key >= len) continue;
+    const int at_key = (kw * NK + x) * 32 + here % 32, key = key0 + at_key;
+    sum[x] += s_sum[at_key];
+    const bool there = key < len && phys_page(c, b, key / ps) >= 0, odd = there && sum[x] != sum[x];
+    again |= odd;
+    if (here >= 32 || key >= len || odd) continue;
     const int64_t at = ((int64_t)b * c.n_kv_heads + g) * cap + key;
     const float before = a.w_in && key < old ? a.w_in[at] : 0.f;
-    a.w_out[at] = phys_page(c, b, key / ps) >= 0 ? before + (sum[x] + s_sum[at_key]) : before;
+    a.w_out[at] = there ? before + sum[x] : before;
   }
+  if (!__any(again)) return;
+#pragma unroll 1
+  for (int x = 0; x < NK; ++x)
+    careful_weights(c, a, s_lse[wave], b, g, key0 + (kw * NK + x) * 32, x == 0 ? sum[0] : sum[NK - 1], here % 32, here / 32);
 }
 
 // Tiles of 128 keys of all sequences and KV heads, the KV head running fastest: a chiplet's L2 then holds the queries of
@@ -281,40 +353,21 @@ void weights_few_kernel(CacheView c, WeightArgs a) {
   }
   const int row0 = chunk_first(a.ch, b), n = chunk_rows(a.ch, b), old = len - n, rows = n * G;
   const float before = a.w_in && key < old && h == 0 ? a.w_in[(int64_t)unit * cap + key] : 0.f;
-  const float sc = kLog2e * 0.08838834764831845f;  // log2(e) / sqrt(128)
-  float sum = 0.f;
   u32x4 kf[8];
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (brought and read by this wavefront alone)
 #pragma unroll
   for (int j = 0; j < 8; ++j) kf[j] = *reinterpret_cast<const u32x4*>(s_k[wave] + col * 256 + (((2 * j + h) ^ (col & 15)) * 16));
-  for (int r0 = max(0, key0 - old) * G / 32 * 32; r0 < rows; r0 += 32) {
-    const int r = min(r0 + col, rows - 1), t = r / G;
-    const int64_t row = (int64_t)(row0 + t) * c.n_q_heads + (int64_t)g * G + (r - t * G);
-    u32x4 qf[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) qf[j] = ld_plain<u32x4>(a.q + row * kHeadDim + h * 8 + j * 16);
-    const float l = a.lse[row];
-    if (h == 0) s_lse[wave][col] = l == -INFINITY || r0 + col >= rows ? INFINITY : l * kLog2e;
-    f32x16 S;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(qf[j]), as_bf16x8(kf[j]), j == 0 ? f32x16{} : S, 0, 0, 0);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (written and read by this wavefront alone)
-    const int first = max(0, key - old) * G - r0 - 4 * h;  // row of the block that sees the key first
-    float part = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const f32x4 rl = *reinterpret_cast<const f32x4*>(&s_lse[wave][2 * i + 4 * h]);
-      float e[4];
-#pragma unroll
-      for (int x = 0; x < 4; ++x) e[x] = 2 * i + x < first ? 0.f : fast_exp2(fmaf(S[i + x], sc, -rl[x]));
-      part += (e[0] + e[1]) + (e[2] + e[3]);
-    }
-    sum += part;
-    asm volatile("" ::: "memory");
+  const auto total_of = [&](auto careful) {
+    const float sum = sum_of_rows<decltype(careful)::value>(c, a, kf, s_lse[wave], g, row0, rows, max(0, key0 - old) * G / 32 * 32,
+                                                            key - old, col, h);
+    const SwapPair sw = swap_rows32(__float_as_uint(sum));
+    return __uint_as_float(sw.a) + __uint_as_float(sw.b);
+  };
+  float total = total_of(std::false_type{});
+  if (__any(pp >= 0 && total != total)) {
+    const float careful = total_of(std::true_type{});
+    if (total != total) total = careful;
   }
-  const SwapPair sw = swap_rows32(__float_as_uint(sum));
-  const float total = __uint_as_float(sw.a) + __uint_as_float(sw.b);
   if (h == 0 && key < len) a.w_out[(int64_t)unit * cap + key] = pp >= 0 ? before + total : before;
 }
 
