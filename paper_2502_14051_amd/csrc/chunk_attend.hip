@@ -582,18 +582,9 @@ ChunkPlan plan_chunk_attend(const CacheView& c, int n_tokens) {
   p.far = c.v_token_major && end * (int64_t)sizeof(bf16_t) >= (int64_t)1 << 32;
   const int64_t held = (int64_t)c.batch * c.pages_cap * c.page_size * c.n_kv_heads * kHeadDim * 2 * (int64_t)sizeof(bf16_t);
   const int64_t rows = (int64_t)n_tokens * c.group / c.batch;  // of a sequence on average
-  // 128 rows to a workgroup, two of which run beside each other out of step, or 256, which share what is read.  The former's
-  // second reading of the keys costs where there are many tiles to read them and the caches do not hold them: 40 shapes
-  // of up to 128 MiB take 10 % less with 128 rows (a prompt of 1024 tokens 32 us, 38 with 256), and so do 16 sequences of up
-  // to 33191 with up to 372 rows each (519 MiB, 112 and 134); 387 tokens of 4 heads behind 131072 (512 MiB) take 1054 us,
-  // 945 with 256, prompts of up to 8191 (192 MiB) 1466 and 1434.  With 64-bit offsets the registers of the former do not suffice.
-  p.tile_rows = !p.far && (rows <= 512 || held <= 128ll << 20) ? 128 : 256;
+  p.tile_rows = chunk_tile_rows(p.far, rows, held);
   p.tile_tokens = p.tile_rows / c.group;
-  // Keys that one tile reads, of caches that the 256 MiB of the last-level cache do not keep until the next call, are read
-  // past the caches: 5 tokens of each of 16 sequences of up to 32768 take 185 us so, 211 without; but 16 tokens behind 4000,
-  // called again at once, 17.8, without 16.5, and where several tiles read the same keys (387 tokens behind 131072, 256 rows
-  // to a tile) 1061, without 946.
-  p.stream = rows <= 128 && !p.far && held > 256ll << 20;
+  p.stream = chunk_past_caches(p.far, rows, held);
   p.slots = 256 * (256 / p.tile_rows);
   const int64_t at_least = ((int64_t)n_tokens + p.tile_tokens - 1) / p.tile_tokens * c.n_kv_heads;
   int64_t tiles = (int64_t)n_tokens / p.tile_tokens + c.batch;

@@ -67,4 +67,20 @@ RKV_HD inline int chunk_part_size(const ChunkLoad& load, int slots, int most, co
   return best;
 }
 
+// Rows of a tile.  `far`: offsets of 64 bits, `rows`: of a sequence on average, `held`: bytes of keys and values there is
+// room for.  128 rows to a workgroup, two of which run beside each other out of step, or 256, which share what is read.  The
+// second reading of the keys costs where many tiles read keys that the caches do not hold (us with 128 rows and with 256,
+// 32 heads over 8): 387 tokens behind 131072 (514 MiB) 1043 and 946, behind 65536 501 and 441, 2048 behind 131072 4289 and
+// 4199, prompts of up to 16384 (192 MiB) 3325 and 3252.  Where they hold them or few tiles read, the finer tiles gain: a
+// prompt of 2048 61.1 and 65.7, 2048 behind 6144 250 and 256, two prompts of up to 4096 198 and 206, 160 tokens behind 40960
+// (161 MiB) 125 and 133.  From 64 to 160 MiB it makes no difference (2048 behind 24576 817 and 817, behind 32768 1064 and
+// 1067).  With 64-bit offsets the registers of the former do not suffice.
+RKV_HD constexpr int chunk_tile_rows(bool far, int64_t rows, int64_t held) { return !far && (rows <= 512 || held <= 128ll << 20) ? 128 : 256; }
+
+// Keys that one tile reads, of caches that the 256 MiB of the last-level cache do not keep until the next call, are read
+// past the caches: 5 tokens of each of 16 sequences of up to 32768 take 185 us so, 211 without; but 16 tokens behind 4000,
+// called again at once, 17.8, without 16.5, and where several tiles read the same keys (387 tokens behind 131072, 256 rows
+// to a tile) 1061, without 946.
+RKV_HD constexpr bool chunk_past_caches(bool far, int64_t rows, int64_t held) { return rows <= 128 && !far && held > 256ll << 20; }
+
 }  // namespace rkv
