@@ -421,7 +421,7 @@ int32_t rocketkv_append_chunk(const rocketkv_cache_t* cache, const rocketkv_chun
 /*
  * Causal attention of a chunk whose tokens are in the cache already: row i of the n rows of sequence b attends to the
  * tokens at positions 0 .. seq_lens[b] - n + i (scale 1/sqrt(head_dim)); bf16 operands, fp32 logits, softmax and sums,
- * bf16 result.  Whole prompts (seq_lens[b] == n), pieces of prompts, turns and single tokens mix freely.
+ * weights rounded to bf16 for their product with the values, bf16 result.  Whole prompts (seq_lens[b] == n), pieces of prompts, turns and single tokens mix freely.
  * q, out: bf16 [n_tokens][n_q_heads][head_dim].  out_lse: optional fp32 [n_tokens][n_q_heads], natural-log sum-exp of the
  * scaled logits.  Absent pages are skipped; a row with nothing to attend to gets zeros and -inf, and one with a logit that
  * is NaN or +inf gets NaN in both.

@@ -12,7 +12,15 @@
 // outputs never leave it, but for one exchange with the lane 32 further, which holds the same row's other keys.  The
 // product leaves a lane the keys of A's rows 8a + 4h + r; with the rows of K read in an order that swaps bits 2 and 3,
 // these are keys 16x + 8h + 0..7, which packed to bf16 are the second product's operand as they stand.  P is rounded to
-// bf16 there (relative 2^-8 at most each, the sum l takes the unrounded values); everything else is fp32.
+// bf16 there (relative 2^-8 at most each; fp32 operands would run at a sixteenth of the matrix rate); everything else is fp32.
+//
+// What that rounding costs is mostly the rows that few keys dominate: their weight's error is the result's.  It cancels where
+// the result is divided by the sum of the rounded weights.  So a row has two sums, l of the weights as they are, which the
+// log sum-exp takes, and lr, in which a unit of keys that outweighs all before it (kept apart for the lane's half of the keys)
+// counts as rounded.  Relative to 64 bits, over all outputs, the cases of 5 to 8191 new tokens are off by 0.0019 to 0.0021 so,
+// by 0.0022 to 0.0023 with l alone, by 0.0017 if the result alone is rounded.  That takes 0 to 2 % of their time (2048 tokens
+// behind 32768 1048 and 1058 us, 6 prompts of up to 8191 1465 and 1490) and 5 % where keys are cut short (100 tokens of each of
+// 2 sequences of 8000, 54.4 and 57.1); every unit counted as rounded is no better (0.0019 to 0.0021) and took 6 to 10 %.
 //
 // What bounds it.  Many rows: the matrix cores and, beside them, the vector instructions of the exponentials, at the clock
 // that the chip's power leaves (2.0 GHz).  2048 tokens of 32 heads behind 32768, 8 KV heads, take 1.04 to 1.09 ms, 1.05 to
@@ -85,6 +93,15 @@ __device__ __forceinline__ float top16(f32x16& s, float c) {
   const float mine = fmaxf(max3(max3(a, b, d), e, f) * c, last);
   const SwapPair sw = swap_rows32(__float_as_uint(mine));
   return fmaxf(__uint_as_float(sw.a), __uint_as_float(sw.b));
+}
+
+// `sum` and two weights as they are after rounding
+__device__ __forceinline__ float add_rounded(uint32_t pair, float sum) {
+#ifdef __HIP_DEVICE_COMPILE__
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3f803f80u), sum, false);
+#else
+  return sum;
+#endif
 }
 
 }  // namespace
@@ -223,7 +240,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
   }
   const int sees_first = working ? pos0 + wave * 32 / G : -1;  // the last key that all of the wavefront's rows see
 
-  // Keys and values of a step to LDS: every wavefront brings 16 tokens of each, 16 bytes a lane.
+  // Keys and values of a step to LDS: every wavefront brings kWaveTok tokens of each, 16 bytes a lane.
   //   keys: [64][16 chunks], chunk x of row r at x ^ r % 16, so that 32 rows at one chunk spread over the banks
   //   values by channel: per page [8 blocks of 16 channels][2 halves of its tokens][16 channels], so that 16 lanes read 256
   //   bytes in a row; by token: [64][16 chunks], chunk x of row r at x ^ 4 (r % 4)
@@ -305,7 +322,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
   };
 
   f32x16 O[4];
-  float m = kNegBig, l = 0.f;
+  float m = kNegBig, l = 0.f, lr = 0.f;
 #pragma unroll
   for (int cb = 0; cb < 4; ++cb) O[cb] = f32x16{};
   const float sc = kLog2e * 0.08838834764831845f;  // log2(e) / sqrt(128)
@@ -355,6 +372,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
     const float mn = up ? mx : m, alpha = fast_exp2(m - mn);
     m = mn;
     l *= alpha;
+    lr *= alpha;
 #pragma unroll
     for (int cb = 0; cb < 4; ++cb) O[cb] *= alpha;
     sum = 0.f;
@@ -459,8 +477,15 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
       fence();
       __builtin_amdgcn_s_setprio(0);
       float sum = ((sums[0] + sums[1]) + (sums[2] + sums[3])) + ((sums[4] + sums[5]) + (sums[6] + sums[7]));
-      if (__any(!(sum <= kSumLimit))) follow_maximum(S, sum, pf);
+      float rounded = sum;
+      if (__any(!(sum <= fminf(kSumLimit, l)))) {
+        if (__any(!(sum <= kSumLimit))) follow_maximum(S, sum, pf);
+        rounded = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) rounded = add_rounded(pf[j / 4][j % 4], rounded);
+      }
       l += sum;
+      lr += rounded;
       if (masked0) keep_future_out(it * kStep + 32 * u, vf, pf);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -497,22 +522,26 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
     if (it + 1 < it1) step(it + 1, std::integral_constant<int, 1>{});
   }
 
-  const SwapPair sw = swap_rows32(__float_as_uint(l));
-  const float sum = __uint_as_float(sw.a) + __uint_as_float(sw.b);
+  const auto both_halves = [](float x) {
+    const SwapPair sw = swap_rows32(__float_as_uint(x));
+    return __uint_as_float(sw.a) + __uint_as_float(sw.b);
+  };
+  const float sum = both_halves(l), rounded = both_halves(lr);
   if (r >= rows) return;
   if (pl.parts > 1) {
     const int64_t at_row = ((int64_t)at * c.n_kv_heads + g) * kRows + r;
     float* part = a.partial + at_row * kHeadDim;
+    const float fit = sum == 0.f ? 0.f : sum / rounded;  // (so that the merge needs one sum)
 #pragma unroll
     for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
       for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<float4*>(part + 32 * cb + 2 * i + 4 * h) = make_float4(O[cb][i], O[cb][i + 1], O[cb][i + 2], O[cb][i + 3]);
+        *reinterpret_cast<float4*>(part + 32 * cb + 2 * i + 4 * h) = make_float4(O[cb][i] * fit, O[cb][i + 1] * fit, O[cb][i + 2] * fit, O[cb][i + 3] * fit);
     if (h == 0) a.part_stats[at_row] = make_float2(m, sum);
     return;
   }
   const int64_t row = packed_row((int)use_late((uint32_t)r));
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;  // (a sum that is NaN stays one, here and below: only 0 is no key at all)
+  const float inv = sum == 0.f ? 0.f : 1.f / rounded;  // (a sum that is NaN stays one, here and below: only 0 is no key at all)
   bf16_t* o = a.out + row * kHeadDim + 4 * h;
 #pragma unroll
   for (int cb = 0; cb < 4; ++cb)
