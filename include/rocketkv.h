@@ -343,8 +343,9 @@ int32_t rocketkv_mt_hsa_decode_append(const rocketkv_cache_t* cache, const rocke
 /*
  * A chunk: the new tokens of all sequences of a cache, packed one behind the other.  Row r of a packed
  * tensor is one token; rows starts[b] .. starts[b+1]-1 belong to sequence b, in order.  A sequence may bring
- * no row, one, or a whole prompt.  starts must ascend from >= 0 to <= n_tokens; rows in front of starts[0] and behind
- * starts[batch] are neither read nor written.  The struct lives in host memory, starts on the device.
+ * no row, one, or a whole prompt.  starts must ascend from >= 0 to <= n_tokens (others read and write nothing out of range,
+ * but results and counters in the workspace are not defined then); rows in front of starts[0] and behind starts[batch] are
+ * neither read nor written.  The struct lives in host memory, starts on the device.
  */
 #define ROCKETKV_MAX_CHUNK (1 << 24)
 typedef struct rocketkv_chunk {

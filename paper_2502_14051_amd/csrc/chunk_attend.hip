@@ -23,7 +23,7 @@
 // 2 sequences of 8000, 54.4 and 57.1); every unit counted as rounded is no better (0.0019 to 0.0021) and took 6 to 10 %.
 //
 // What bounds it.  Many rows: the matrix cores and, beside them, the vector instructions of the exponentials, at the clock
-// that the chip's power leaves (2.0 GHz).  2048 tokens of 32 heads behind 32768, 8 KV heads, take 1.04 to 1.09 ms, 1.05 to
+// that the chip's power leaves (2.0 GHz).  2048 tokens of 32 heads behind 32768, 8 KV heads, take 1.04 to 1.12 ms, 1.01 to
 // 1.09 PFLOP/s, the matrix cores busy 52 % of the cycles; without loads and LDS reads the same instructions ran at 1.30, a
 // library's product of 8192^3 runs at 1.40.  Few rows: HBM, 6.2 TB/s for 5 tokens of each of 16 sequences of up to 32768.
 // Why 32 rows to a wavefront and two wavefronts to a SIMD: one stands at its products while the other forms exponentials.

@@ -6,7 +6,7 @@
 // are merged by a second launch.  A part is not free: its rows' sums go to memory and come back, and it begins with steps
 // that overlap nothing; together what kChunkPartSteps steps of its work take.
 // (For a prompt alone, whose last tile sees twice the mean, parts of the long tiles only were no gain either: 2048 tokens
-// 80 us so, 68 whole.)
+// 80 us so, 62 whole.)
 #pragma once
 #include <stdint.h>
 

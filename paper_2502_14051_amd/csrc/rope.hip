@@ -173,7 +173,7 @@ __device__ __forceinline__ NewTokens new_tokens(const CacheView& c, const ChunkV
 
 // New tokens into the cache, in one launch: the first workgroups take blocks of `pages` pages (aligned to `pages`, a multiple
 // of eight, so that a channel's summaries leave as whole 16-byte pieces) of some heads, the others blocks of query rows (with
-// the two kinds mixed instead, 131072 tokens took 711 us, so 668).  A block is worked through kBlockTokens tokens at a time: sines of the tokens, then head by head the key rows
+// the two kinds mixed instead, 131072 tokens take 797 us, so 706).  A block is worked through kBlockTokens tokens at a time: sines of the tokens, then head by head the key rows
 // (turned) and the value rows to the pools and to LDS, from where a thread takes a pair of channels down the tokens of a
 // page: extremes of the keys, in the order of the tokens as single appends would fold them, and the 16 values of a
 // channel-major tile's row.

@@ -11,8 +11,8 @@
 // sums do not depend on the order of workgroups.
 //
 // What bounds it: as the attention, the matrix cores and the exponentials beside them (a product fewer, so more of the
-// latter: 2048 tokens of 32 heads over 34816 keys and 8 KV heads 598 us, 0.95 PFLOP/s); with few rows the one reading of
-// the keys (one token of each of 16 sequences of 4123: 29 us, 4.8 TB/s, launch included).
+// latter: 2048 tokens of 32 heads over 34816 keys and 8 KV heads 612 to 650 us by machine, 0.87 to 0.93 PFLOP/s); with few
+// rows the one reading of the keys (one token of each of 16 sequences of 4123: 29 us, 4.8 TB/s, launch included).
 #include <type_traits>
 
 #include "attend_core.h"
@@ -302,7 +302,7 @@ __device__ __forceinline__ void weights_of_keys(const CacheView& c, const Weight
 // Tiles of 128 keys of all sequences and KV heads, the KV head running fastest: a chiplet's L2 then holds the queries of
 // one head, if there are as many.  What the last round of workgroups over the chip leaves idle, if that is half of it or
 // more, halves of the last tiles fill (us, without and with: 2048 tokens of 32 heads over 34816 keys and 8 KV heads, four
-// and a quarter rounds, 625 and 598, 0.95 PFLOP/s; 1186 tokens of 64 heads over 2242, a quarter of a round, 123 and 77).
+// and a quarter rounds, 625 and 598; 1186 tokens of 64 heads over 2242, a quarter of a round, 123 and 77).
 // Other tiles took longer: 256 keys to a workgroup of four wavefronts 673, to one of eight 705, half tiles only 743.
 __global__ __launch_bounds__(kWeightWaves * kWave) __attribute__((amdgpu_waves_per_eu(2)))
 void weights_kernel(CacheView c, WeightArgs a) {
@@ -384,6 +384,11 @@ hipError_t launch_weights(const CacheView& c, const ChunkView& ch, const bf16_t*
   a.w_in = w_in;
   a.w_out = w_out;
   const unsigned units = (unsigned)(c.batch * c.n_kv_heads), tiles = (unsigned)((c.pages_cap * c.page_size + kTileKeys - 1) / kTileKeys);
+  // By the rows of a sequence on average (us by the form for few and by the other, 32 heads over 8): 8 tokens, 32 rows, of one
+  // sequence of 32000 20.6 and 34.3, of 16 of 4000 33.8 and 66.9, of 64 119.6 and 261.8; 64 rows 27.5 and 34.4, 47.8 and 67.4,
+  // 162 and 262; 128 rows 40.7 and 34.4, 75.3 and 67.3, 262 and 267.  The line lies at 32, below what equal sequences ask for, as
+  // the rows may as well be one sequence's: 449 tokens beside 63 single ones, all over 4000, take 274 and 281, but 2048 beside
+  // 80, 105 rows a sequence, 995 and 462.
   if ((int64_t)ch.n_tokens * c.group <= 32ll * c.batch) hipLaunchKernelGGL(weights_few_kernel, dim3(tiles, units), dim3(kFewT), 0, st, c, a);
   else hipLaunchKernelGGL(weights_kernel, dim3((unsigned)weights_workgroups(c)), dim3(kWeightWaves * kWave), 0, st, c, a);
   return hipGetLastError();
