@@ -96,3 +96,22 @@ def test_a_key(lens, news):
             c.cache.k_pool[b * c.cache.pages_cap + t // 16, :, t % 16, 9] = NAN
             c.K[b, :, t, 9] = NAN
     assert check(c, lse, w) > 0
+
+
+@pytest.mark.parametrize("lens,news,ps,token_major", [([18000], [40], 16, False), ([18000, 900], [200, 3], 3, True), ([300, 50], [5, 1], 5, True),
+                                                      ([9000, 9500], [70, 130], 64, True)])
+def test_all_of_them_over_scattered_pages(lens, news, ps, token_major):
+    """Whole tiles of keys and halves of them, with pages absent."""
+    c = ref.Case(74, lens, news, 8, 2, ps, token_major, pad=(1, 1))
+    lse = ref.attention(c)[1].float()
+    w = torch.rand((len(lens), 2, c.cache.pages_cap * ps), generator=torch.Generator().manual_seed(74)).cuda()
+    for b, (n, new) in enumerate(zip(lens, news)):
+        first = c.starts[b]
+        lse[first + new // 2, 3] = NAN
+        c.q[first, 6], lse[first, 6] = INF, -INF
+        c.q[first + new - 1, 5], lse[first + new - 1, 5] = NAN, -INF
+        for t, bad in ((n // 5, NAN), (n // 2, INF), (n - 1, NAN)):
+            c.cache.k_pool[c.cache.block_table[b, t // ps].long(), 0, t % ps, 77] = bad
+            c.K[b, 0, t, 77] = bad
+    c.drop_pages([(0, 1), (0, lens[0] // (3 * ps)), (len(lens) - 1, 2)])
+    assert check(c, lse, w) > 0
