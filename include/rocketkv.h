@@ -469,6 +469,152 @@ int32_t rocketkv_weight_evict(const rocketkv_cache_t* src, const float* weights,
                               size_t workspace_bytes, void* stream);
 
 /*
+ * Quantised caches: keys and values in 8 or 4 bits.  Of a token's 128 channels every block of 32 has a power of two of its
+ * own, and channel c is the value of its code times 2^(scale - 127), scale the byte of block c / 32:
+ *   E4M3  a byte a channel: sign, 4 bits of exponent (bias 7), 3 of mantissa; largest value 448
+ *   E2M1  four bits a channel, channel 2i in the low half of byte i: sign, 2 bits of exponent (bias 1), 1 of mantissa;
+ *         values 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * A block's power of two is the smallest with which none of its values exceeds the largest code (2^-100 at least, and at
+ * most what keeps values in the range of bf16: 2^119 for E4M3, 2^125 for E2M1, beyond which codes are the largest); a value
+ * becomes the nearest code, half way the even one.  A block that holds a value that is not finite becomes NaN as a whole,
+ * scale 255; other scales lie in 27 .. 252.  Every value a code stands for is a bf16 value, so a quantised cache is exactly
+ * the bf16 cache of those values in half or a quarter of the bytes, and what an operator computes on it is what its
+ * counterpart computes on that cache.
+ *
+ * Both keys and values lie by token.  In each of the four pools token t of a physical page pp and KV head g is entry
+ *        pp * stride_page + g * stride_head + t
+ * strides counted in tokens and the same for all four: rows of 128 (E4M3) or 64 bytes (E2M1) in the pools of codes, of 4
+ * bytes in those of scales.  Everything else is as in rocketkv_cache_t; page_size 1..64.  Page summaries are of the keys as
+ * the cache holds them, in the layout above.
+ */
+typedef enum {
+  ROCKETKV_Q_E4M3 = 0,
+  ROCKETKV_Q_E2M1 = 1
+} rocketkv_q_format_t;
+
+typedef struct rocketkv_qcache {
+  int32_t batch;
+  int32_t n_q_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t page_size;
+  int32_t pages_cap;
+  int64_t n_phys_pages;
+  int64_t stride_page;        /* tokens between physical pages; all pages and heads below 2^32 tokens */
+  int64_t stride_head;        /* tokens between KV heads inside a page, >= page_size */
+  int32_t* seq_lens;
+  const int32_t* block_table; /* device [batch][pages_cap] or NULL (identity) */
+  void* k_codes;              /* device, 16-byte aligned */
+  void* v_codes;
+  uint8_t* k_scales;          /* device, 4-byte aligned */
+  uint8_t* v_scales;
+  int32_t format;             /* rocketkv_q_format_t */
+} rocketkv_qcache_t;
+
+/*
+ * Scratch bytes of the calls on a quantised cache (0 on an invalid request), by the same names as for the others:
+ * ROCKETKV_OP_APPEND_CHUNK and ROCKETKV_OP_CHUNK_ATTEND (a = n_tokens), ROCKETKV_OP_ATTEND (a = pages_row_len, 0 = every
+ * page), ROCKETKV_OP_HSA_DECODE (a = token_budget).
+ */
+size_t rocketkv_q_workspace_bytes(int32_t op, const rocketkv_qcache_t* cache, int32_t a);
+
+/*
+ * rocketkv_append_chunk into a quantised cache: keys are turned in fp32 and quantised from there, values from bf16.
+ * Arguments and rules as there; kmax / kmin follow the keys as the cache holds them.
+ */
+int32_t rocketkv_q_append_chunk(const rocketkv_qcache_t* cache, const rocketkv_chunk_t* chunk, const rocketkv_rope_t* rope,
+                                const int32_t* positions, const void* q, int64_t q_stride, void* q_out, const void* k_new,
+                                int64_t k_stride, const void* v_new, int64_t v_stride, void* kmax, void* kmin,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Which tokens of a chunk each of them sees, in place of those up to its own: row i of a sequence's rows sees its row j if
+ * bit j % 32 of word j / 32 of its words is set (rows from 32 * words on are seen by none), itself only if its own bit is.
+ * What the cache held before the chunk is seen by all.  Trees of drafted tokens, and any other pattern.
+ * bits: device uint32 [n_tokens][words].  The struct lives in host memory.
+ */
+typedef struct rocketkv_mask {
+  const uint32_t* bits;
+  int32_t words;
+} rocketkv_mask_t;
+
+/*
+ * The mask of trees of drafted tokens: each sees itself, its parent, that one's parent and so on.
+ * parents: device int32 [n_tokens], a row's parent as an index among its sequence's rows, smaller than its own; anything
+ *          else (-1): it continues the cache itself.
+ * bits: device uint32 [n_tokens][words], written; words at least what the sequence with the most rows needs to have all of
+ *       them seen, ceil(rows / 32).
+ * base, positions: both or neither; positions int32 [n_tokens] becomes base[b] + the number of ancestors, which with the
+ *       lengths before the tokens are appended is the position each would have on its path (the positions of
+ *       rocketkv_append_chunk).  base: device int32 [batch].
+ * Rows of no sequence are left as they were.
+ */
+int32_t rocketkv_tree_mask(int32_t batch, const rocketkv_chunk_t* chunk, const int32_t* parents, const int32_t* base,
+                           uint32_t* bits, int32_t words, int32_t* positions, void* stream);
+
+/*
+ * rocketkv_chunk_attend with `mask` in place of the order of the chunk's tokens.  A row that sees nothing gets zeros and
+ * -inf.  Keys and values that a row does not see may be anything.
+ * workspace: rocketkv_workspace_bytes(ROCKETKV_OP_CHUNK_ATTEND, cache, n_tokens, 0).
+ */
+int32_t rocketkv_masked_attend(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const rocketkv_mask_t* mask,
+                               const void* q, void* out, float* out_lse, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/*
+ * rocketkv_chunk_attend (mask NULL) or rocketkv_masked_attend over a quantised cache.
+ * workspace: rocketkv_q_workspace_bytes(ROCKETKV_OP_CHUNK_ATTEND, cache, n_tokens).
+ */
+int32_t rocketkv_q_chunk_attend(const rocketkv_qcache_t* cache, const rocketkv_chunk_t* chunk, const rocketkv_mask_t* mask,
+                                const void* q, void* out, float* out_lse, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/*
+ * rocketkv_attend over a quantised cache: one token per sequence over the listed pages of each KV head (NULL: every page).
+ * A page may be listed more than once; its tokens then count as often.
+ * workspace: rocketkv_q_workspace_bytes(ROCKETKV_OP_ATTEND, cache, pages_row_len).
+ */
+int32_t rocketkv_q_attend(const rocketkv_qcache_t* cache, const void* q, const int32_t* pages, int32_t pages_row_len,
+                          void* out, float* out_lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * rocketkv_hsa_decode over a quantised cache: the selection of rocketkv_hsa_select by the summaries, then rocketkv_q_attend
+ * over the selected pages.
+ * workspace: rocketkv_q_workspace_bytes(ROCKETKV_OP_HSA_DECODE, cache, token_budget).
+ */
+int32_t rocketkv_q_hsa_decode(const rocketkv_qcache_t* cache, const void* q, const void* kmax, const void* kmin,
+                              int32_t channel_budget, int32_t token_budget, int32_t n_recent_pages, void* out,
+                              float* out_lse, int32_t* out_pages, int32_t* out_channels, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/*
+ * A bf16 cache into a quantised one, and a quantised one back into bf16 (which is exact): tokens 0 .. src->seq_lens[b] - 1
+ * of every sequence, dst->seq_lens[b] = src->seq_lens[b].  The same batch and KV heads; page sizes, tables, strides and the
+ * layout of values are each cache's own (channel-major: page_size 16).  A sequence longer than either cache counts as empty.
+ * A token of an absent page of src becomes zeros; one of an absent page of dst goes nowhere.  A channel-major dst gets
+ * whole tiles, zeros behind the last token.
+ */
+int32_t rocketkv_quantise(const rocketkv_cache_t* src, const rocketkv_qcache_t* dst, void* stream);
+int32_t rocketkv_restore(const rocketkv_qcache_t* src, const rocketkv_cache_t* dst, void* stream);
+
+/*
+ * Of the chunk appended last, the tokens whose `keep` is not 0 stay, moved together in their order behind what the cache
+ * held before; the others are dropped.  With n rows of which m are kept, seq_lens[b] becomes seq_lens[b] - n + m.  (After
+ * the verification of a draft: the accepted path of a tree, or the accepted beginning of a sequence.)
+ * keep: device uint8 [n_tokens].
+ * kmax, kmin: both, or both NULL; the columns from the page of the first of the n rows on are computed anew, over all keys
+ *       of these pages.  A sequence without rows is left as it is.
+ * A sequence with more rows than tokens is left unchanged.  A token moved from an absent page leaves zeros, one moved to
+ * an absent page goes nowhere; absent pages count for no summary.
+ * Channel-major V needs page_size 16.
+ * workspace: rocketkv_workspace_bytes(ROCKETKV_OP_APPEND_CHUNK, cache, n_tokens, 0), or rocketkv_q_workspace_bytes.
+ */
+int32_t rocketkv_keep_tokens(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const uint8_t* keep, void* kmax,
+                             void* kmin, void* workspace, size_t workspace_bytes, void* stream);
+int32_t rocketkv_q_keep_tokens(const rocketkv_qcache_t* cache, const rocketkv_chunk_t* chunk, const uint8_t* keep,
+                               void* kmax, void* kmin, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Adaptive compression decomposition (Section 3.6): for a sequence of seq_len
  * tokens and a total token budget t (memory traffic of one attention call in
  * key/value pairs, Step 2 and Step 3 together), c = seq_len / t (at least 1),

@@ -819,6 +819,30 @@ RopeView rope_of(const rocketkv_rope_t* r) {
   return v;
 }
 
+// Arguments of the append of a chunk beside the cache.
+int check_append(int n_q_heads, int n_kv_heads, const rocketkv_chunk_t* chunk, const rocketkv_rope_t* rope,
+                 const int32_t* positions, const void* q, int64_t q_stride, const void* q_out, const void* k_new,
+                 int64_t k_stride, const void* v_new, int64_t v_stride, const void* kmax, const void* kmin,
+                 const void* workspace, size_t workspace_bytes, const char* who) {
+  if (int r = check_chunk(chunk, who)) return r;
+  if (rope)
+    if (int r = check_rope(rope, who)) return r;
+  if (positions && !rope) return fail(ROCKETKV_INVALID_ARG, "%s: positions without rope", who);
+  if (!q != !q_out) return fail(ROCKETKV_INVALID_ARG, "%s: q and q_out go together", who);
+  if (q) {
+    if (int r = check_rows(q, q_stride, n_q_heads, "q", who)) return r;
+    if (int r = check_rows(q_out, (int64_t)n_q_heads * kHeadDim, n_q_heads, "q_out", who)) return r;
+    if (q == q_out && q_stride != (int64_t)n_q_heads * kHeadDim)
+      return fail(ROCKETKV_INVALID_ARG, "%s: in place needs equal strides", who);
+  }
+  if (int r = check_rows(k_new, k_stride, n_kv_heads, "k_new", who)) return r;
+  if (int r = check_rows(v_new, v_stride, n_kv_heads, "v_new", who)) return r;
+  if (!kmax != !kmin) return fail(ROCKETKV_INVALID_ARG, "%s: kmax and kmin go together", who);
+  if (((uintptr_t)kmax | (uintptr_t)kmin) & 15)
+    return fail(ROCKETKV_INVALID_ARG, "%s: kmax / kmin must be 16-byte aligned", who);
+  return check_workspace(workspace, workspace_bytes, ROCKETKV_WS_HEADER_BYTES, who);
+}
+
 ChunkView chunk_of(const rocketkv_chunk_t* ch) { return {ch->n_tokens, ch->starts}; }
 
 }  // namespace
@@ -887,23 +911,8 @@ int32_t rocketkv_append_chunk(const rocketkv_cache_t* cache, const rocketkv_chun
   const char* who = "rocketkv_append_chunk";
   if (int r = check_cache(cache, true, who)) return r;
   if (int r = check_attend_shape(cache, who)) return r;
-  if (int r = check_chunk(chunk, who)) return r;
-  if (rope)
-    if (int r = check_rope(rope, who)) return r;
-  if (positions && !rope) return fail(ROCKETKV_INVALID_ARG, "%s: positions without rope", who);
-  if (!q != !q_out) return fail(ROCKETKV_INVALID_ARG, "%s: q and q_out go together", who);
-  if (q) {
-    if (int r = check_rows(q, q_stride, cache->n_q_heads, "q", who)) return r;
-    if (int r = check_rows(q_out, (int64_t)cache->n_q_heads * kHeadDim, cache->n_q_heads, "q_out", who)) return r;
-    if (q == q_out && q_stride != (int64_t)cache->n_q_heads * kHeadDim)
-      return fail(ROCKETKV_INVALID_ARG, "%s: in place needs equal strides", who);
-  }
-  if (int r = check_rows(k_new, k_stride, cache->n_kv_heads, "k_new", who)) return r;
-  if (int r = check_rows(v_new, v_stride, cache->n_kv_heads, "v_new", who)) return r;
-  if (!kmax != !kmin) return fail(ROCKETKV_INVALID_ARG, "%s: kmax and kmin go together", who);
-  if (((uintptr_t)kmax | (uintptr_t)kmin) & 15)
-    return fail(ROCKETKV_INVALID_ARG, "%s: kmax / kmin must be 16-byte aligned", who);
-  if (int r = check_workspace(workspace, workspace_bytes, ROCKETKV_WS_HEADER_BYTES, who)) return r;
+  if (int r = check_append(cache->n_q_heads, cache->n_kv_heads, chunk, rope, positions, q, q_stride, q_out, k_new, k_stride, v_new,
+                           v_stride, kmax, kmin, workspace, workspace_bytes, who)) return r;
   const hipError_t e = launch_append_chunk(
       view_of(cache), chunk_of(chunk), rope_of(rope), positions, static_cast<const bf16_t*>(q), q_stride,
       static_cast<bf16_t*>(q_out), static_cast<const bf16_t*>(k_new), k_stride, static_cast<const bf16_t*>(v_new), v_stride,
@@ -911,10 +920,11 @@ int32_t rocketkv_append_chunk(const rocketkv_cache_t* cache, const rocketkv_chun
   return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
 }
 
-int32_t rocketkv_chunk_attend(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const void* q, void* out,
-                              float* out_lse, void* workspace, size_t workspace_bytes, void* stream) {
-  g_err[0] = 0;
-  const char* who = "rocketkv_chunk_attend";
+namespace {
+
+// Shared body of rocketkv_chunk_attend and rocketkv_masked_attend.
+int chunk_attend_impl(const char* who, const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const MaskView& mask,
+                      const void* q, void* out, float* out_lse, void* workspace, size_t workspace_bytes, void* stream) {
   if (int r = check_cache(cache, true, who)) return r;
   if (int r = check_attend_shape(cache, who)) return r;
   if (int r = check_chunk(chunk, who)) return r;
@@ -926,9 +936,17 @@ int32_t rocketkv_chunk_attend(const rocketkv_cache_t* cache, const rocketkv_chun
   const ChunkPlan plan = plan_chunk_attend(v, chunk->n_tokens);
   if (plan.workgroups * 512 > 0xffffffffll) return fail(ROCKETKV_UNSUPPORTED, "%s: too many rows for one launch", who);
   if (int r = check_workspace(workspace, workspace_bytes, plan.total_bytes, who)) return r;
-  const hipError_t e = launch_chunk_attend(v, chunk_of(chunk), static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out),
+  const hipError_t e = launch_chunk_attend(v, chunk_of(chunk), mask, static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out),
                                            out_lse, workspace, plan, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
+}
+
+}  // namespace
+
+int32_t rocketkv_chunk_attend(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const void* q, void* out,
+                              float* out_lse, void* workspace, size_t workspace_bytes, void* stream) {
+  g_err[0] = 0;
+  return chunk_attend_impl("rocketkv_chunk_attend", cache, chunk, {nullptr, 0}, q, out, out_lse, workspace, workspace_bytes, stream);
 }
 
 int32_t rocketkv_accumulate_weights(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const void* q,
@@ -975,6 +993,309 @@ int32_t rocketkv_weight_evict(const rocketkv_cache_t* src, const float* weights,
   if (int r = check_workspace(workspace, workspace_bytes, plan.total_bytes, who)) return r;
   const hipError_t e = launch_evict(sv, weights, n_recent, keep_budget, dv, dst_weights, kept_idx, workspace, plan,
                                     static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
+}
+
+}  // extern "C"
+
+// ---- quantised caches, and trees of drafted tokens -------------------------------------------------------
+
+namespace {
+
+// The part that a quantised cache has in common with others, checked as they are.
+rocketkv_cache_t common_part(const rocketkv_qcache_t* c) {
+  rocketkv_cache_t v;
+  memset(&v, 0, sizeof v);
+  v.batch = c->batch;
+  v.n_q_heads = c->n_q_heads;
+  v.n_kv_heads = c->n_kv_heads;
+  v.head_dim = c->head_dim;
+  v.page_size = c->page_size;
+  v.pages_cap = c->pages_cap;
+  v.n_phys_pages = c->n_phys_pages;
+  v.stride_page = c->stride_page;
+  v.stride_head = c->stride_head;
+  v.seq_lens = c->seq_lens;
+  v.block_table = c->block_table;
+  v.k_pool = c->k_codes;
+  v.v_pool = c->v_codes;
+  v.v_layout = ROCKETKV_V_TOKEN_MAJOR;
+  return v;
+}
+
+int check_qcache(const rocketkv_qcache_t* c, bool need_pools, const char* who) {
+  if (!c) return fail(ROCKETKV_INVALID_ARG, "%s: cache is NULL", who);
+  const rocketkv_cache_t part = common_part(c);
+  if (int r = check_cache(&part, false, who)) return r;
+  if (c->format != ROCKETKV_Q_E4M3 && c->format != ROCKETKV_Q_E2M1)
+    return fail(ROCKETKV_INVALID_ARG, "%s: unknown format %d", who, c->format);
+  if (!need_pools) return ROCKETKV_OK;
+  if (!c->seq_lens || !c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales)
+    return fail(ROCKETKV_INVALID_ARG, "%s: seq_lens / codes / scales must not be NULL", who);
+  if (c->n_phys_pages < 1) return fail(ROCKETKV_INVALID_ARG, "%s: n_phys_pages must be positive", who);
+  if (c->stride_head < c->page_size || c->stride_page / c->n_kv_heads < c->page_size)
+    return fail(ROCKETKV_INVALID_ARG, "%s: strides must hold page_size tokens a head and n_kv_heads * page_size a page", who);
+  const int64_t most = 4294967295ll;  // tokens that 32 bits count, as the kernels do
+  if (c->n_phys_pages > 2147483647ll || c->stride_page > most / c->n_phys_pages || c->stride_head > most / c->n_kv_heads ||
+      c->n_phys_pages * c->stride_page + c->n_kv_heads * c->stride_head > most)
+    return fail(ROCKETKV_UNSUPPORTED, "%s: n_phys_pages * stride_page must stay below 2^32 tokens", who);
+  if (!c->block_table && c->n_phys_pages < (int64_t)c->batch * c->pages_cap)
+    return fail(ROCKETKV_INVALID_ARG, "%s: identity block table needs n_phys_pages >= batch * pages_cap", who);
+  if (((uintptr_t)c->k_codes | (uintptr_t)c->v_codes) & 15)
+    return fail(ROCKETKV_INVALID_ARG, "%s: codes must be 16-byte aligned", who);
+  if (((uintptr_t)c->k_scales | (uintptr_t)c->v_scales) & 3)
+    return fail(ROCKETKV_INVALID_ARG, "%s: scales must be 4-byte aligned", who);
+  return ROCKETKV_OK;
+}
+
+QCacheView q_view_of(const rocketkv_qcache_t* c) {
+  const rocketkv_cache_t part = common_part(c);
+  return {view_of(&part), c->k_scales, c->v_scales, c->format};
+}
+
+int check_n_tokens(int32_t n, const char* who) {
+  if (n < 0) return fail(ROCKETKV_INVALID_ARG, "%s: n_tokens must be >= 0", who);
+  if (n > ROCKETKV_MAX_CHUNK) return fail(ROCKETKV_UNSUPPORTED, "%s: n_tokens %d exceeds %d", who, n, ROCKETKV_MAX_CHUNK);
+  return ROCKETKV_OK;
+}
+
+// `words` of masks that are read or written
+int check_mask(const uint32_t* bits, int32_t words, const char* who) {
+  if (!bits) return fail(ROCKETKV_INVALID_ARG, "%s: mask->bits must not be NULL", who);
+  if ((uintptr_t)bits & 3) return fail(ROCKETKV_INVALID_ARG, "%s: mask->bits must be 4-byte aligned", who);
+  if (words < 1) return fail(ROCKETKV_INVALID_ARG, "%s: words must be >= 1", who);
+  if (words > ROCKETKV_MAX_CHUNK / 32) return fail(ROCKETKV_UNSUPPORTED, "%s: words %d exceeds %d", who, words, ROCKETKV_MAX_CHUNK / 32);
+  return ROCKETKV_OK;
+}
+
+int check_list(const rocketkv_qcache_t* c, int32_t row_len, const char* who) {
+  if ((int64_t)row_len * c->page_size > (int64_t)1 << 30)
+    return fail(ROCKETKV_UNSUPPORTED, "%s: pages_row_len * page_size exceeds 2^30", who);
+  return ROCKETKV_OK;
+}
+
+struct QDecodePlan {
+  ChunkPlan attend;
+  int row_len;
+  size_t list_off, scores_off, total;
+};
+QDecodePlan plan_q_decode(const rocketkv_qcache_t* c, int T) {
+  QDecodePlan d;
+  const rocketkv_cache_t part = common_part(c);
+  d.row_len = list_len_for_budget(&part, T);
+  d.attend = plan_q_list(q_view_of(c), d.row_len);
+  const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  d.list_off = up(d.attend.total_bytes);
+  d.scores_off = d.list_off + up((size_t)c->batch * c->n_kv_heads * d.row_len * sizeof(int32_t));
+  d.total = d.scores_off + up((size_t)c->batch * c->n_kv_heads * c->pages_cap * sizeof(float));
+  return d;
+}
+
+// Pools, scales and lengths of both sides of a conversion
+int check_convert(const rocketkv_cache_t* bf16, const rocketkv_qcache_t* codes, const char* who) {
+  if (int r = check_cache(bf16, true, who)) return r;
+  if (int r = check_qcache(codes, true, who)) return r;
+  if (int r = check_attend_shape(bf16, who)) return r;
+  if (bf16->batch != codes->batch || bf16->n_kv_heads != codes->n_kv_heads)
+    return fail(ROCKETKV_INVALID_ARG, "%s: src and dst must agree on batch and KV heads", who);
+  if (bf16->seq_lens == codes->seq_lens || bf16->k_pool == codes->k_codes || bf16->v_pool == codes->v_codes)
+    return fail(ROCKETKV_INVALID_ARG, "%s: src and dst pools and lengths must be distinct", who);
+  if (convert_workgroups(view_of(bf16), q_view_of(codes)) * 256 > 0xffffffffll)
+    return fail(ROCKETKV_UNSUPPORTED, "%s: too many tokens for one launch", who);
+  return ROCKETKV_OK;
+}
+
+// Arguments of the keeping of tokens beside the cache
+int check_keep(const rocketkv_chunk_t* chunk, const void* keep, const void* kmax, const void* kmin, const void* ws, size_t have,
+               const char* who) {
+  if (int r = check_chunk(chunk, who)) return r;
+  if (!keep && chunk->n_tokens > 0) return fail(ROCKETKV_INVALID_ARG, "%s: keep must not be NULL", who);
+  if (!kmax != !kmin) return fail(ROCKETKV_INVALID_ARG, "%s: kmax and kmin go together", who);
+  if (((uintptr_t)kmax | (uintptr_t)kmin) & 15) return fail(ROCKETKV_INVALID_ARG, "%s: kmax / kmin must be 16-byte aligned", who);
+  return check_workspace(ws, have, ROCKETKV_WS_HEADER_BYTES, who);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t rocketkv_q_workspace_bytes(int32_t op, const rocketkv_qcache_t* cache, int32_t a) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_q_workspace_bytes";
+  if (check_qcache(cache, false, who)) return 0;
+  switch (op) {
+    case ROCKETKV_OP_APPEND_CHUNK:
+    case ROCKETKV_OP_CHUNK_ATTEND:
+      if (check_n_tokens(a, who)) return 0;
+      return op == ROCKETKV_OP_APPEND_CHUNK ? (size_t)ROCKETKV_WS_HEADER_BYTES : plan_q_attend(q_view_of(cache), a).total_bytes;
+    case ROCKETKV_OP_ATTEND:
+      if (a < 0) { fail(ROCKETKV_INVALID_ARG, "%s: pages_row_len must be >= 0", who); return 0; }
+      if (check_list(cache, a, who)) return 0;
+      return plan_q_list(q_view_of(cache), a ? a : cache->pages_cap).total_bytes;
+    case ROCKETKV_OP_HSA_DECODE:
+      if (a < 1) { fail(ROCKETKV_INVALID_ARG, "%s: token_budget must be >= 1", who); return 0; }
+      return plan_q_decode(cache, a).total;
+    default:
+      fail(ROCKETKV_INVALID_ARG, "%s: unknown op %d", who, op);
+      return 0;
+  }
+}
+
+int32_t rocketkv_q_append_chunk(const rocketkv_qcache_t* cache, const rocketkv_chunk_t* chunk, const rocketkv_rope_t* rope,
+                                const int32_t* positions, const void* q, int64_t q_stride, void* q_out, const void* k_new,
+                                int64_t k_stride, const void* v_new, int64_t v_stride, void* kmax, void* kmin,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_q_append_chunk";
+  if (int r = check_qcache(cache, true, who)) return r;
+  if (int r = check_append(cache->n_q_heads, cache->n_kv_heads, chunk, rope, positions, q, q_stride, q_out, k_new, k_stride, v_new,
+                           v_stride, kmax, kmin, workspace, workspace_bytes, who)) return r;
+  const hipError_t e = launch_q_append(
+      q_view_of(cache), chunk_of(chunk), rope_of(rope), positions, static_cast<const bf16_t*>(q), q_stride,
+      static_cast<bf16_t*>(q_out), static_cast<const bf16_t*>(k_new), k_stride, static_cast<const bf16_t*>(v_new), v_stride,
+      static_cast<bf16_t*>(kmax), static_cast<bf16_t*>(kmin), workspace, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
+}
+
+int32_t rocketkv_tree_mask(int32_t batch, const rocketkv_chunk_t* chunk, const int32_t* parents, const int32_t* base,
+                           uint32_t* bits, int32_t words, int32_t* positions, void* stream) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_tree_mask";
+  if (batch < 1) return fail(ROCKETKV_INVALID_ARG, "%s: batch must be positive", who);
+  if (int r = check_chunk(chunk, who)) return r;
+  if (!parents && chunk->n_tokens > 0) return fail(ROCKETKV_INVALID_ARG, "%s: parents must not be NULL", who);
+  if (!base != !positions) return fail(ROCKETKV_INVALID_ARG, "%s: base and positions go together", who);
+  if (int r = check_mask(bits, words, who)) return r;
+  const hipError_t e = launch_tree_mask(batch, chunk_of(chunk), parents, base, bits, words, positions,
+                                        static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
+}
+
+int32_t rocketkv_masked_attend(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const rocketkv_mask_t* mask,
+                               const void* q, void* out, float* out_lse, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_masked_attend";
+  if (!mask) return fail(ROCKETKV_INVALID_ARG, "%s: mask is NULL", who);
+  if (int r = check_mask(mask->bits, mask->words, who)) return r;
+  return chunk_attend_impl(who, cache, chunk, {mask->bits, mask->words}, q, out, out_lse, workspace, workspace_bytes, stream);
+}
+
+int32_t rocketkv_q_chunk_attend(const rocketkv_qcache_t* cache, const rocketkv_chunk_t* chunk, const rocketkv_mask_t* mask,
+                                const void* q, void* out, float* out_lse, void* workspace, size_t workspace_bytes,
+                                void* stream) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_q_chunk_attend";
+  if (int r = check_qcache(cache, true, who)) return r;
+  if (int r = check_chunk(chunk, who)) return r;
+  if (mask)
+    if (int r = check_mask(mask->bits, mask->words, who)) return r;
+  const int64_t stride = (int64_t)cache->n_q_heads * kHeadDim;
+  if (int r = check_rows(q, stride, cache->n_q_heads, "q", who)) return r;
+  if (int r = check_rows(out, stride, cache->n_q_heads, "out", who)) return r;
+  if (q == out) return fail(ROCKETKV_INVALID_ARG, "%s: q and out must be distinct", who);
+  const QCacheView v = q_view_of(cache);
+  const ChunkPlan plan = plan_q_attend(v, chunk->n_tokens);
+  if (plan.workgroups * 512 > 0xffffffffll) return fail(ROCKETKV_UNSUPPORTED, "%s: too many rows for one launch", who);
+  if (int r = check_workspace(workspace, workspace_bytes, plan.total_bytes, who)) return r;
+  const hipError_t e = launch_q_attend(v, chunk_of(chunk), mask ? MaskView{mask->bits, mask->words} : MaskView{nullptr, 0},
+                                       static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out), out_lse, workspace, plan,
+                                       static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
+}
+
+int32_t rocketkv_q_attend(const rocketkv_qcache_t* cache, const void* q, const int32_t* pages, int32_t pages_row_len,
+                          void* out, float* out_lse, void* workspace, size_t workspace_bytes, void* stream) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_q_attend";
+  if (int r = check_qcache(cache, true, who)) return r;
+  const int64_t stride = (int64_t)cache->n_q_heads * kHeadDim;
+  if (int r = check_rows(q, stride, cache->n_q_heads, "q", who)) return r;
+  if (int r = check_rows(out, stride, cache->n_q_heads, "out", who)) return r;
+  if (q == out) return fail(ROCKETKV_INVALID_ARG, "%s: q and out must be distinct", who);
+  if (pages && pages_row_len < 1) return fail(ROCKETKV_INVALID_ARG, "%s: pages_row_len must be >= 1", who);
+  const int row_len = pages ? pages_row_len : cache->pages_cap;
+  if (int r = check_list(cache, row_len, who)) return r;
+  const QCacheView v = q_view_of(cache);
+  const ChunkPlan plan = plan_q_list(v, row_len);
+  if (int r = check_workspace(workspace, workspace_bytes, plan.total_bytes, who)) return r;
+  const hipError_t e = launch_q_list(v, pages, row_len, static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out), out_lse,
+                                     workspace, plan, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
+}
+
+int32_t rocketkv_q_hsa_decode(const rocketkv_qcache_t* cache, const void* q, const void* kmax, const void* kmin,
+                              int32_t channel_budget, int32_t token_budget, int32_t n_recent_pages, void* out,
+                              float* out_lse, int32_t* out_pages, int32_t* out_channels, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_q_hsa_decode";
+  if (int r = check_qcache(cache, true, who)) return r;
+  const rocketkv_cache_t part = common_part(cache);
+  if (int r = check_select_args(&part, q, kmax, kmin, channel_budget, token_budget, n_recent_pages, who)) return r;
+  if (int r = check_rows(out, (int64_t)cache->n_q_heads * kHeadDim, cache->n_q_heads, "out", who)) return r;
+  if (q == out) return fail(ROCKETKV_INVALID_ARG, "%s: q and out must be distinct", who);
+  const QDecodePlan d = plan_q_decode(cache, token_budget);
+  if (int r = check_workspace(workspace, workspace_bytes, d.total, who)) return r;
+  const QCacheView v = q_view_of(cache);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  SelectArgs a;
+  a.q = static_cast<const bf16_t*>(q);
+  a.kmax = static_cast<const bf16_t*>(kmax);
+  a.kmin = static_cast<const bf16_t*>(kmin);
+  a.k1 = channel_budget;
+  a.T = token_budget;
+  a.n_recent = n_recent_pages;
+  a.out_pages = reinterpret_cast<int32_t*>(ws + d.list_off);
+  a.row_len = d.row_len;
+  a.out_pages2 = out_pages;
+  a.row_len2 = d.row_len;
+  a.out_channels = out_channels;
+  a.out_scores = select_wants_split(v.tokens, a.k1) ? reinterpret_cast<float*>(ws + d.scores_off) : nullptr;
+  a.in_scores = nullptr;
+  hipError_t e = launch_hsa_select(v.tokens, a, st);
+  if (e != hipSuccess) return hip_fail(e, who);
+  e = launch_q_list(v, a.out_pages, d.row_len, a.q, static_cast<bf16_t*>(out), out_lse, ws, d.attend, st);
+  return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
+}
+
+int32_t rocketkv_quantise(const rocketkv_cache_t* src, const rocketkv_qcache_t* dst, void* stream) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_quantise";
+  if (int r = check_convert(src, dst, who)) return r;
+  const hipError_t e = launch_quantise(view_of(src), q_view_of(dst), static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
+}
+
+int32_t rocketkv_restore(const rocketkv_qcache_t* src, const rocketkv_cache_t* dst, void* stream) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_restore";
+  if (int r = check_convert(dst, src, who)) return r;
+  const hipError_t e = launch_restore(q_view_of(src), view_of(dst), static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
+}
+
+int32_t rocketkv_keep_tokens(const rocketkv_cache_t* cache, const rocketkv_chunk_t* chunk, const uint8_t* keep, void* kmax,
+                             void* kmin, void* workspace, size_t workspace_bytes, void* stream) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_keep_tokens";
+  if (int r = check_cache(cache, true, who)) return r;
+  if (int r = check_attend_shape(cache, who)) return r;
+  if (int r = check_keep(chunk, keep, kmax, kmin, workspace, workspace_bytes, who)) return r;
+  const hipError_t e = launch_keep(view_of(cache), chunk_of(chunk), keep, static_cast<bf16_t*>(kmax), static_cast<bf16_t*>(kmin),
+                                   workspace, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
+}
+
+int32_t rocketkv_q_keep_tokens(const rocketkv_qcache_t* cache, const rocketkv_chunk_t* chunk, const uint8_t* keep,
+                               void* kmax, void* kmin, void* workspace, size_t workspace_bytes, void* stream) {
+  g_err[0] = 0;
+  const char* who = "rocketkv_q_keep_tokens";
+  if (int r = check_qcache(cache, true, who)) return r;
+  if (int r = check_keep(chunk, keep, kmax, kmin, workspace, workspace_bytes, who)) return r;
+  const hipError_t e = launch_q_keep(q_view_of(cache), chunk_of(chunk), keep, static_cast<bf16_t*>(kmax),
+                                     static_cast<bf16_t*>(kmin), workspace, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ROCKETKV_OK : hip_fail(e, who);
 }
 

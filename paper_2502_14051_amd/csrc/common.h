@@ -409,8 +409,47 @@ struct ChunkPlan {
   size_t total_bytes;
 };
 ChunkPlan plan_chunk_attend(const CacheView& c, int n_tokens);
-hipError_t launch_chunk_attend(const CacheView& c, const ChunkView& ch, const bf16_t* q, bf16_t* out, float* out_lse,
-                               void* ws, const ChunkPlan& plan, hipStream_t st);
+// Which tokens of the chunk its rows see; null: those up to their own.
+struct MaskView {
+  const uint32_t* bits;
+  int32_t words;
+};
+hipError_t launch_chunk_attend(const CacheView& c, const ChunkView& ch, const MaskView& mask, const bf16_t* q, bf16_t* out,
+                               float* out_lse, void* ws, const ChunkPlan& plan, hipStream_t st);
+void plan_chunk_tiles(const CacheView& c, int n_tokens, ChunkPlan& p);  // what follows from p.tile_rows
+struct ChunkAttendArgs;
+ChunkAttendArgs chunk_attend_args(const ChunkView& ch, const bf16_t* q, bf16_t* out, float* out_lse, void* ws,
+                                  const ChunkPlan& plan);
+hipError_t launch_chunk_merge(const CacheView& c, const ChunkAttendArgs& a, const ChunkPlan& plan, hipStream_t st);
+
+// ---- quantised caches ----
+// A token's key and value are 128 codes each, by token, and a byte per block of 32 channels, the block's power of two + 127.
+constexpr int kBlockChannels = 32;
+struct QCacheView {
+  CacheView tokens;  // strides and offsets in tokens, the pools those of the codes
+  uint8_t *k_scales, *v_scales;
+  int32_t format;    // rocketkv_q_format_t
+};
+ChunkPlan plan_q_attend(const QCacheView& c, int n_tokens);
+hipError_t launch_q_attend(const QCacheView& c, const ChunkView& ch, const MaskView& mask, const bf16_t* q, bf16_t* out,
+                           float* out_lse, void* ws, const ChunkPlan& plan, hipStream_t st);
+ChunkPlan plan_q_list(const QCacheView& c, int row_len);
+hipError_t launch_q_list(const QCacheView& c, const int32_t* pages, int row_len, const bf16_t* q, bf16_t* out, float* out_lse,
+                         void* ws, const ChunkPlan& plan, hipStream_t st);
+hipError_t launch_q_append(const QCacheView& c, const ChunkView& ch, const RopeView& r, const int32_t* positions,
+                           const bf16_t* q, int64_t q_stride, bf16_t* q_out, const bf16_t* k, int64_t k_stride,
+                           const bf16_t* v, int64_t v_stride, bf16_t* kmax, bf16_t* kmin, void* ws, hipStream_t st);
+int64_t convert_workgroups(const CacheView& bf16, const QCacheView& codes);
+hipError_t launch_quantise(const CacheView& src, const QCacheView& dst, hipStream_t st);
+hipError_t launch_restore(const QCacheView& src, const CacheView& dst, hipStream_t st);
+
+// ---- trees of drafted tokens ----
+hipError_t launch_tree_mask(int batch, const ChunkView& ch, const int32_t* parents, const int32_t* base, uint32_t* bits,
+                            int words, int32_t* positions, hipStream_t st);
+hipError_t launch_keep(const CacheView& c, const ChunkView& ch, const uint8_t* keep, bf16_t* kmax, bf16_t* kmin, void* ws,
+                       hipStream_t st);
+hipError_t launch_q_keep(const QCacheView& c, const ChunkView& ch, const uint8_t* keep, bf16_t* kmax, bf16_t* kmin, void* ws,
+                         hipStream_t st);
 int64_t weights_workgroups(const CacheView& c);  // at most
 hipError_t launch_weights(const CacheView& c, const ChunkView& ch, const bf16_t* q, const float* lse, const float* w_in,
                           float* w_out, hipStream_t st);

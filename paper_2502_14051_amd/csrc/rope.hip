@@ -9,6 +9,7 @@
 // Both kernels are bound by memory: every head row is read and written once.  What would cost more than that, the sines,
 // is computed once per token and pair into LDS and used by all heads a workgroup handles.
 #include "common.h"
+#include "quantise.h"
 
 namespace rkv {
 
@@ -91,10 +92,10 @@ __device__ __forceinline__ RowPart request_row(const RopeView& r, const bf16_t* 
   return p;
 }
 inline bool rope_is_odd(const RopeView& r) { return !r.interleaved && r.rot_dim % 16 != 0; }
-// rounded to bf16 once, at the end
-__device__ __forceinline__ uint4 turn_row(const RopeView& r, const RowPart& p, const float2* cs, int c0) {
+__device__ __forceinline__ Eight turn8(const RopeView& r, const RowPart& p, const float2* cs, int c0) {
   const Eight a = unpack8(p.own);
-  float y[8];
+  Eight out;
+  float (&y)[8] = out.x;
   if (r.interleaved) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -114,7 +115,12 @@ __device__ __forceinline__ uint4 turn_row(const RopeView& r, const RowPart& p, c
       y[e] = in ? a.x[e] * t.x + (low ? -f.x[e] : f.x[e]) * t.y : a.x[e];
     }
   }
-  return make_uint4(pack2(y[0], y[1]), pack2(y[2], y[3]), pack2(y[4], y[5]), pack2(y[6], y[7]));
+  return out;
+}
+// rounded to bf16 once, at the end
+__device__ __forceinline__ uint4 turn_row(const RopeView& r, const RowPart& p, const float2* cs, int c0) {
+  const Eight y = turn8(r, p, cs, c0);
+  return make_uint4(pack2(y.x[0], y.x[1]), pack2(y.x[2], y.x[3]), pack2(y.x[4], y.x[5]), pack2(y.x[6], y.x[7]));
 }
 
 // `n` tokens of `heads` heads each, from x (rows of x_stride elements a token) to y, by the whole workgroup; the
@@ -176,7 +182,7 @@ __device__ __forceinline__ NewTokens new_tokens(const CacheView& c, const ChunkV
 // the two kinds mixed instead, 131072 tokens take 797 us, so 706).  A block is worked through kBlockTokens tokens at a time: sines of the tokens, then head by head the key rows
 // (turned) and the value rows to the pools and to LDS, from where a thread takes a pair of channels down the tokens of a
 // page: extremes of the keys, in the order of the tokens as single appends would fold them, and the 16 values of a
-// channel-major tile's row.
+// channel-major tile's row.  Quantised caches take codes instead, by token, and LDS the values these stand for.
 struct AppendChunkArgs {
   ChunkView ch;
   RopeView rope;              // rot_dim 0: nothing is turned
@@ -186,10 +192,12 @@ struct AppendChunkArgs {
   bf16_t *q_out, *kmax, *kmin;  // kmax null: no summaries
   int pages, kv_wgs, heads_per_wg, head_groups, q_block;
   uint32_t* arrived;  // per sequence at read_slot(): workgroups that have read its length
+  uint8_t *k_scales, *v_scales;  // of a quantised cache
 };
 
-template <bool ODD>
-__global__ __launch_bounds__(kRopeT) __attribute__((amdgpu_waves_per_eu(ODD ? 3 : 4)))
+// FMT: of a quantised cache, whose pools and strides `c` then holds; or kBf16.
+template <bool ODD, int FMT>
+__global__ __launch_bounds__(kRopeT) __attribute__((amdgpu_waves_per_eu(ODD || FMT != kBf16 ? 3 : 4)))
 void append_chunk_kernel(CacheView c, AppendChunkArgs a) {
   extern __shared__ __align__(16) unsigned char s_mem[];
   float2* s_cs = reinterpret_cast<float2*>(s_mem);                                                    // [tokens][pairs]
@@ -252,7 +260,19 @@ void append_chunk_kernel(CacheView c, AppendChunkArgs a) {
 #pragma unroll
         for (int u = 0; u < kPasses; ++u) {
           const int i = i0 + u * kRowsPerPass, t = tl + i;
-          if (t < th) {
+          if constexpr (FMT != kBf16) {
+            if (t < th) {
+              const Codes8 k = quantise8<FMT>(turns ? turn8(a.rope, kp[u], s_cs + i * half, c0).x : unpack8(kp[u].own).x);
+              const Codes8 v = quantise8<FMT>(unpack8(vp[u]).x);
+              if (a.kmax) *reinterpret_cast<uint4*>(s_k + i * (kHeadDim / 2) + c0 / 2) = restore8<FMT>(k.codes, k.scale);
+              const int64_t pp = phys_page(c, b, t / ps);
+              if (pp >= 0) {
+                const int64_t at = pp * c.stride_page + g * c.stride_head + t % ps;
+                store_codes<FMT>(c.k_pool, a.k_scales, at, c0 / 8, k);
+                store_codes<FMT>(c.v_pool, a.v_scales, at, c0 / 8, v);
+              }
+            }
+          } else if (t < th) {
             const uint4 k = turns ? turn_row(a.rope, kp[u], s_cs + i * half, c0) : kp[u].own;
             *reinterpret_cast<uint4*>(s_k + i * (kHeadDim / 2) + c0 / 2) = k;
             if (!c.v_token_major) *reinterpret_cast<uint4*>(s_v + i * (kHeadDim / 2) + c0 / 2) = vp[u];
@@ -373,11 +393,17 @@ hipError_t launch_rope(const RopeView& r, const int32_t* positions, int n_tokens
   return hipGetLastError();
 }
 
-hipError_t launch_append_chunk(const CacheView& c, const ChunkView& ch, const RopeView& r, const int32_t* positions,
-                               const bf16_t* q, int64_t q_stride, bf16_t* q_out, const bf16_t* k, int64_t k_stride,
-                               const bf16_t* v, int64_t v_stride, bf16_t* kmax, bf16_t* kmin, void* ws, hipStream_t st) {
+namespace {
+
+template <int FMT>
+hipError_t launch_append_any(const CacheView& c, uint8_t* k_scales, uint8_t* v_scales, const ChunkView& ch, const RopeView& r,
+                             const int32_t* positions, const bf16_t* q, int64_t q_stride, bf16_t* q_out, const bf16_t* k,
+                             int64_t k_stride, const bf16_t* v, int64_t v_stride, bf16_t* kmax, bf16_t* kmin, void* ws,
+                             hipStream_t st) {
   if (ch.n_tokens == 0) return hipSuccess;
   AppendChunkArgs a;
+  a.k_scales = k_scales;
+  a.v_scales = v_scales;
   a.ch = ch;
   a.rope = r;
   a.positions = positions;
@@ -411,8 +437,25 @@ hipError_t launch_append_chunk(const CacheView& c, const ChunkView& ch, const Ro
   const size_t lds = (size_t)kBlockTokens * kHeadDim / 2 * sizeof(float2) + 2 * (size_t)kBlockTokens * kHeadDim * sizeof(bf16_t) +
                      (kmax ? (size_t)a.heads_per_wg * 2 * kHeadDim * pages * sizeof(bf16_t) : 0);
   const int n_kv = a.kv_wgs * a.head_groups;
-  hipLaunchKernelGGL(rope_is_odd(r) ? append_chunk_kernel<true> : append_chunk_kernel<false>, dim3(n_kv + q_wgs), dim3(kRopeT), lds, st, c, a);
+  const auto kernel = rope_is_odd(r) ? append_chunk_kernel<true, FMT> : append_chunk_kernel<false, FMT>;
+  hipLaunchKernelGGL(kernel, dim3(n_kv + q_wgs), dim3(kRopeT), lds, st, c, a);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_append_chunk(const CacheView& c, const ChunkView& ch, const RopeView& r, const int32_t* positions,
+                               const bf16_t* q, int64_t q_stride, bf16_t* q_out, const bf16_t* k, int64_t k_stride,
+                               const bf16_t* v, int64_t v_stride, bf16_t* kmax, bf16_t* kmin, void* ws, hipStream_t st) {
+  return launch_append_any<kBf16>(c, nullptr, nullptr, ch, r, positions, q, q_stride, q_out, k, k_stride, v, v_stride, kmax,
+                                  kmin, ws, st);
+}
+
+hipError_t launch_q_append(const QCacheView& c, const ChunkView& ch, const RopeView& r, const int32_t* positions,
+                           const bf16_t* q, int64_t q_stride, bf16_t* q_out, const bf16_t* k, int64_t k_stride,
+                           const bf16_t* v, int64_t v_stride, bf16_t* kmax, bf16_t* kmin, void* ws, hipStream_t st) {
+  return (c.format == ROCKETKV_Q_E4M3 ? launch_append_any<ROCKETKV_Q_E4M3> : launch_append_any<ROCKETKV_Q_E2M1>)(
+      c.tokens, c.k_scales, c.v_scales, ch, r, positions, q, q_stride, q_out, k, k_stride, v, v_stride, kmax, kmin, ws, st);
 }
 
 }  // namespace rkv

@@ -23,6 +23,7 @@ ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3, 4
 MAX_CHUNK = 1 << 24
 MAX_PAGES = 32768
 V_CHANNEL_MAJOR, V_TOKEN_MAJOR = 0, 1
+Q_E4M3, Q_E2M1 = 0, 1
 
 EXPORTS = [
     "rocketkv_workspace_bytes", "rocketkv_workspace_init", "rocketkv_build_page_summaries", "rocketkv_hsa_select",
@@ -34,6 +35,9 @@ EXPORTS = [
     "rocketkv_stream_gather", "rocketkv_stream_gather_sink_bytes",
     "rocketkv_rope_frequencies", "rocketkv_rope", "rocketkv_append_chunk", "rocketkv_chunk_attend",
     "rocketkv_accumulate_weights", "rocketkv_weight_evict",
+    "rocketkv_q_workspace_bytes", "rocketkv_q_append_chunk", "rocketkv_q_chunk_attend", "rocketkv_q_attend",
+    "rocketkv_q_hsa_decode", "rocketkv_quantise", "rocketkv_restore", "rocketkv_tree_mask", "rocketkv_masked_attend",
+    "rocketkv_keep_tokens", "rocketkv_q_keep_tokens",
 ]
 NOALLOC_SCRATCH_BYTES = 4 << 20
 
@@ -53,6 +57,23 @@ class CacheStruct(C.Structure):
         ("seq_lens", C.c_void_p), ("block_table", C.c_void_p),
         ("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("v_layout", C.c_int32),
     ]
+
+
+class QCacheStruct(C.Structure):
+    """Mirror of ``rocketkv_qcache_t``."""
+    _fields_ = [
+        ("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+        ("head_dim", C.c_int32), ("page_size", C.c_int32), ("pages_cap", C.c_int32),
+        ("n_phys_pages", C.c_int64), ("stride_page", C.c_int64), ("stride_head", C.c_int64),
+        ("seq_lens", C.c_void_p), ("block_table", C.c_void_p),
+        ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+        ("format", C.c_int32),
+    ]
+
+
+class MaskStruct(C.Structure):
+    """Mirror of ``rocketkv_mask_t``."""
+    _fields_ = [("bits", C.c_void_p), ("words", C.c_int32)]
 
 
 class IndexStruct(C.Structure):
@@ -149,6 +170,29 @@ def lib():
         L.rocketkv_accumulate_weights.argtypes = [cp, hp, vp, vp, vp, vp, vp]
         L.rocketkv_weight_evict.restype = i32
         L.rocketkv_weight_evict.argtypes = [cp, vp, i32, i32, cp, vp, vp, vp, sz, vp]
+        qp, mp = C.POINTER(QCacheStruct), C.POINTER(MaskStruct)
+        L.rocketkv_q_workspace_bytes.restype = sz
+        L.rocketkv_q_workspace_bytes.argtypes = [i32, qp, i32]
+        L.rocketkv_q_append_chunk.restype = i32
+        L.rocketkv_q_append_chunk.argtypes = [qp, hp, rp, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+        L.rocketkv_q_chunk_attend.restype = i32
+        L.rocketkv_q_chunk_attend.argtypes = [qp, hp, mp, vp, vp, vp, vp, sz, vp]
+        L.rocketkv_q_attend.restype = i32
+        L.rocketkv_q_attend.argtypes = [qp, vp, vp, i32, vp, vp, vp, sz, vp]
+        L.rocketkv_q_hsa_decode.restype = i32
+        L.rocketkv_q_hsa_decode.argtypes = [qp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.rocketkv_quantise.restype = i32
+        L.rocketkv_quantise.argtypes = [cp, qp, vp]
+        L.rocketkv_restore.restype = i32
+        L.rocketkv_restore.argtypes = [qp, cp, vp]
+        L.rocketkv_tree_mask.restype = i32
+        L.rocketkv_tree_mask.argtypes = [i32, hp, vp, vp, vp, i32, vp, vp]
+        L.rocketkv_masked_attend.restype = i32
+        L.rocketkv_masked_attend.argtypes = [cp, hp, mp, vp, vp, vp, vp, sz, vp]
+        L.rocketkv_keep_tokens.restype = i32
+        L.rocketkv_keep_tokens.argtypes = [cp, hp, vp, vp, vp, vp, sz, vp]
+        L.rocketkv_q_keep_tokens.restype = i32
+        L.rocketkv_q_keep_tokens.argtypes = [qp, hp, vp, vp, vp, vp, sz, vp]
         L.rocketkv_decompose.restype = i32
         L.rocketkv_decompose.argtypes = [C.c_int64, i32, i32, C.POINTER(SplitStruct)]
         L.rocketkv_last_error.restype = C.c_char_p
@@ -554,6 +598,11 @@ def rope(rope: Rope, positions, x, y, stream=None):
 def append_chunk(cache: Cache, chunk: Chunk, k_new, v_new, kmax, kmin, workspace, rope: Optional[Rope] = None,
                  positions=None, q=None, q_out=None, stream=None):
     """k_new, v_new: bf16 [n_tokens][n_kv_heads][128], q: bf16 [n_tokens][n_q_heads][128], tokens at any stride."""
+    _append(lib().rocketkv_append_chunk, _here_with, cache, chunk, k_new, v_new, kmax, kmin, workspace, rope, positions, q, q_out,
+            stream)
+
+
+def _append(call, here, cache, chunk, k_new, v_new, kmax, kmin, workspace, rope, positions, q, q_out, stream):
     n = chunk.n_tokens
     _tensor("k_new", k_new, "bfloat16", (n, cache.n_kv_heads, 128), rows=True)
     _tensor("v_new", v_new, "bfloat16", (n, cache.n_kv_heads, 128), rows=True)
@@ -565,15 +614,14 @@ def append_chunk(cache: Cache, chunk: Chunk, k_new, v_new, kmax, kmin, workspace
         _tensor("positions", positions, "int32", (n,))
     _summaries(cache, kmax, kmin)
     st, ch, r = cache.struct(), chunk.struct(cache), rope.struct() if rope is not None else None
-    _here_with(cache, k_new=k_new, v_new=v_new, q=q, q_out=q_out, positions=positions, kmax=kmax, kmin=kmin,
-               starts=chunk.starts, inv_freq=rope.inv_freq if rope is not None else None, workspace=workspace)
+    here(cache, k_new=k_new, v_new=v_new, q=q, q_out=q_out, positions=positions, kmax=kmax, kmin=kmin,
+         starts=chunk.starts, inv_freq=rope.inv_freq if rope is not None else None, workspace=workspace)
     if n == 0:
         return
     stride = lambda t, heads: t.stride(0) if n > 1 and t is not None else heads * 128
-    _check(lib().rocketkv_append_chunk(C.byref(st), C.byref(ch), C.byref(r) if r is not None else None, _ptr(positions),
-                                       _ptr(q), stride(q, cache.n_q_heads), _ptr(q_out), _ptr(k_new),
-                                       stride(k_new, cache.n_kv_heads), _ptr(v_new), stride(v_new, cache.n_kv_heads),
-                                       _ptr(kmax), _ptr(kmin), _ptr(workspace), workspace.numel(), _stream(stream)))
+    _check(call(C.byref(st), C.byref(ch), C.byref(r) if r is not None else None, _ptr(positions), _ptr(q),
+                stride(q, cache.n_q_heads), _ptr(q_out), _ptr(k_new), stride(k_new, cache.n_kv_heads), _ptr(v_new),
+                stride(v_new, cache.n_kv_heads), _ptr(kmax), _ptr(kmin), _ptr(workspace), workspace.numel(), _stream(stream)))
 
 
 def _summaries(cache, kmax, kmin):
@@ -635,6 +683,226 @@ def weight_evict(src: Cache, weights, n_recent: int, keep_budget: int, dst: Cach
     _here_with(dst)
     _check(lib().rocketkv_weight_evict(C.byref(s), _ptr(weights), n_recent, keep_budget, C.byref(d), _ptr(dst_weights),
                                        _ptr(kept_idx), _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+@dataclass
+class QCache:
+    """A paged cache of quantised keys and values in torch tensors, plus its C descriptor (see rocketkv_qcache_t).
+
+    k_codes, v_codes: uint8 [n_phys_pages][n_kv_heads][page_size][128], or [..][64] in Q_E2M1
+    k_scales, v_scales: uint8 [n_phys_pages][n_kv_heads][page_size][4]
+    Pages and heads may lie at any stride, counted in tokens and the same for all four; a page's tokens are contiguous.
+    seq_lens: int32 [batch]; block_table: int32 [batch][pages_cap] or None (identity).
+    """
+    batch: int
+    n_q_heads: int
+    n_kv_heads: int
+    head_dim: int
+    page_size: int
+    pages_cap: int
+    k_codes: object
+    v_codes: object
+    k_scales: object
+    v_scales: object
+    seq_lens: object
+    block_table: object = None
+    format: int = Q_E4M3
+
+    def struct(self) -> QCacheStruct:
+        width = q_row_bytes(self.format)
+        stride_page, stride_head = self.k_scales.stride()[:2]
+        shape = (self.k_codes.shape[0], self.n_kv_heads, self.page_size)
+        for name, t, w in (("k_codes", self.k_codes, width), ("v_codes", self.v_codes, width), ("k_scales", self.k_scales, 4),
+                           ("v_scales", self.v_scales, 4)):
+            if t.element_size() != 1 or t.shape != shape + (w,):
+                raise RocketKVError(INVALID_ARG, f"{name}: need bytes {shape + (w,)}, got {t.dtype} {tuple(t.shape)}")
+            if t.stride() != (stride_page // 4 * w, stride_head // 4 * w, w, 1):
+                raise RocketKVError(INVALID_ARG, f"{name}: strides must be those of k_scales in tokens, rows contiguous")
+        table = self.block_table
+        return QCacheStruct(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_size, self.pages_cap,
+                            shape[0], stride_page // 4, stride_head // 4, _ptr(self.seq_lens),
+                            None if table is None else table.data_ptr(), self.k_codes.data_ptr(), self.v_codes.data_ptr(),
+                            self.k_scales.data_ptr(), self.v_scales.data_ptr(), self.format)
+
+
+def q_row_bytes(format: int) -> int:
+    """Bytes of a token's codes of one head."""
+    if format not in (Q_E4M3, Q_E2M1):
+        raise RocketKVError(INVALID_ARG, f"unknown format {format}")
+    return 128 if format == Q_E4M3 else 64
+
+
+def alloc_qcache(batch, n_q_heads, n_kv_heads, page_size, pages_cap, device, format=Q_E4M3, block_table=None,
+                 n_phys_pages=None) -> QCache:
+    """An empty quantised cache."""
+    import torch
+    pages_cap = (pages_cap + 7) // 8 * 8
+    n_phys = n_phys_pages if n_phys_pages is not None else batch * pages_cap
+    mk = lambda width: torch.empty((n_phys, n_kv_heads, page_size, width), dtype=torch.uint8, device=device)
+    width = q_row_bytes(format)
+    return QCache(batch, n_q_heads, n_kv_heads, 128, page_size, pages_cap, mk(width), mk(width), mk(4), mk(4),
+                  torch.zeros((batch,), dtype=torch.int32, device=device), block_table, format)
+
+
+def _here_with_q(cache, **tensors):
+    _here(k_codes=cache.k_codes, v_codes=cache.v_codes, k_scales=cache.k_scales, v_scales=cache.v_scales,
+          seq_lens=cache.seq_lens, block_table=cache.block_table, **tensors)
+
+
+def q_workspace_bytes(op: int, cache: QCache, a: int = 0) -> int:
+    st = cache.struct()
+    n = lib().rocketkv_q_workspace_bytes(op, C.byref(st), a)
+    if n == 0 and last_error():
+        raise RocketKVError(INVALID_ARG, last_error())
+    return int(n)
+
+
+def q_alloc_workspace(op: int, cache: QCache, a: int = 0, stream=None):
+    """Allocate (torch) and initialise a workspace for `op` on a quantised cache."""
+    import torch
+    ws = torch.empty((max(q_workspace_bytes(op, cache, a), 256),), dtype=torch.uint8, device=cache.k_codes.device)
+    workspace_init(ws, stream)
+    return ws
+
+
+def q_append_chunk(cache: QCache, chunk: Chunk, k_new, v_new, kmax, kmin, workspace, rope: Optional[Rope] = None,
+                   positions=None, q=None, q_out=None, stream=None):
+    """append_chunk into a quantised cache."""
+    _append(lib().rocketkv_q_append_chunk, _here_with_q, cache, chunk, k_new, v_new, kmax, kmin, workspace, rope, positions, q,
+            q_out, stream)
+
+
+@dataclass
+class Mask:
+    """Which of its sequence's rows each row of a chunk sees: bits, int32 [n_tokens][words] (see rocketkv_mask_t)."""
+    bits: object
+
+    def struct(self, n: int) -> MaskStruct:
+        _tensor("bits", self.bits, "int32", (n, self.bits.shape[-1]))
+        return MaskStruct(_ptr(self.bits), int(self.bits.shape[1]))
+
+
+def alloc_mask(n_tokens: int, most_rows: int, device) -> Mask:
+    """A mask for chunks of n_tokens, of sequences that bring at most most_rows each."""
+    import torch
+    return Mask(torch.zeros((n_tokens, max(1, (most_rows + 31) // 32)), dtype=torch.int32, device=device))
+
+
+def tree_mask(chunk: Chunk, parents, mask: Mask, base=None, positions=None, stream=None):
+    """parents: int32 [n_tokens]; base: int32 [batch] and positions: int32 [n_tokens], or None; see rocketkv_tree_mask."""
+    n, batch = chunk.n_tokens, int(chunk.starts.shape[0]) - 1
+    _tensor("starts", chunk.starts, "int32", (batch + 1,))
+    _tensor("parents", parents, "int32", (n,))
+    if base is not None:
+        _tensor("base", base, "int32", (batch,))
+    if positions is not None:
+        _tensor("positions", positions, "int32", (n,))
+    m = mask.struct(n)
+    _here(starts=chunk.starts, parents=parents, bits=mask.bits, base=base, positions=positions)
+    if n == 0:
+        return
+    ch = ChunkStruct(n, _ptr(chunk.starts))
+    _check(lib().rocketkv_tree_mask(batch, C.byref(ch), _ptr(parents), _ptr(base), m.bits, m.words, _ptr(positions),
+                                    _stream(stream)))
+
+
+def _attend_tensors(n, cache, q, out, out_lse):
+    _tensor("q", q, "bfloat16", (n, cache.n_q_heads, 128))
+    _tensor("out", out, "bfloat16", (n, cache.n_q_heads, 128))
+    if out_lse is not None:
+        _tensor("out_lse", out_lse, "float32", (n, cache.n_q_heads))
+
+
+def masked_attend(cache: Cache, chunk: Chunk, mask: Mask, q, out, out_lse, workspace, stream=None):
+    """chunk_attend with `mask` in place of the order of the chunk's tokens."""
+    n = chunk.n_tokens
+    _attend_tensors(n, cache, q, out, out_lse)
+    st, ch, m = cache.struct(), chunk.struct(cache), mask.struct(n)
+    _here_with(cache, q=q, out=out, out_lse=out_lse, starts=chunk.starts, bits=mask.bits, workspace=workspace)
+    if n == 0:
+        return
+    _check(lib().rocketkv_masked_attend(C.byref(st), C.byref(ch), C.byref(m), _ptr(q), _ptr(out), _ptr(out_lse),
+                                        _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+def q_chunk_attend(cache: QCache, chunk: Chunk, q, out, out_lse, workspace, mask: Optional[Mask] = None, stream=None):
+    """chunk_attend, or with a mask masked_attend, over a quantised cache."""
+    n = chunk.n_tokens
+    _attend_tensors(n, cache, q, out, out_lse)
+    st, ch, m = cache.struct(), chunk.struct(cache), mask.struct(n) if mask is not None else None
+    _here_with_q(cache, q=q, out=out, out_lse=out_lse, starts=chunk.starts, bits=mask.bits if mask is not None else None,
+                 workspace=workspace)
+    if n == 0:
+        return
+    _check(lib().rocketkv_q_chunk_attend(C.byref(st), C.byref(ch), C.byref(m) if m is not None else None, _ptr(q), _ptr(out),
+                                         _ptr(out_lse), _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+def q_attend(cache: QCache, q, pages, out, out_lse, workspace, stream=None):
+    """q, out: bf16 [batch][n_q_heads][128]; pages: int32 [batch][n_kv_heads][row_len] or None (every page)."""
+    _attend_tensors(cache.batch, cache, q, out, out_lse)
+    if pages is not None:
+        _tensor("pages", pages, "int32", (cache.batch, cache.n_kv_heads, pages.shape[-1]))
+    st = cache.struct()
+    _here_with_q(cache, q=q, pages=pages, out=out, out_lse=out_lse, workspace=workspace)
+    _check(lib().rocketkv_q_attend(C.byref(st), _ptr(q), _ptr(pages), 0 if pages is None else int(pages.shape[-1]), _ptr(out),
+                                   _ptr(out_lse), _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+def q_hsa_decode(cache: QCache, q, kmax, kmin, channel_budget: int, token_budget: int, n_recent_pages: int, out, out_lse,
+                 out_pages, out_channels, workspace, stream=None):
+    """hsa_decode over a quantised cache."""
+    _attend_tensors(cache.batch, cache, q, out, out_lse)
+    _summaries(cache, kmax, kmin)
+    if out_pages is not None:
+        _tensor("out_pages", out_pages, "int32", (cache.batch, cache.n_kv_heads, pages_row_len(cache, token_budget)))
+    if out_channels is not None:
+        _tensor("out_channels", out_channels, "int32", (cache.batch, cache.n_kv_heads, channel_budget))
+    st = cache.struct()
+    _here_with_q(cache, q=q, kmax=kmax, kmin=kmin, out=out, out_lse=out_lse, out_pages=out_pages, out_channels=out_channels,
+                 workspace=workspace)
+    _check(lib().rocketkv_q_hsa_decode(C.byref(st), _ptr(q), _ptr(kmax), _ptr(kmin), channel_budget, token_budget,
+                                       n_recent_pages, _ptr(out), _ptr(out_lse), _ptr(out_pages), _ptr(out_channels),
+                                       _ptr(workspace), workspace.numel(), _stream(stream)))
+
+
+def quantise(src: Cache, dst: QCache, stream=None):
+    """Every token of a bf16 cache into a quantised one."""
+    s, d = src.struct(), dst.struct()
+    _here_with(src)
+    _here_with_q(dst)
+    _check(lib().rocketkv_quantise(C.byref(s), C.byref(d), _stream(stream)))
+
+
+def restore(src: QCache, dst: Cache, stream=None):
+    """Every token of a quantised cache into a bf16 one, exactly."""
+    s, d = src.struct(), dst.struct()
+    _here_with_q(src)
+    _here_with(dst)
+    _check(lib().rocketkv_restore(C.byref(s), C.byref(d), _stream(stream)))
+
+
+def _keep(call, here, cache, chunk, keep, kmax, kmin, workspace, stream):
+    n = chunk.n_tokens
+    if keep.element_size() != 1 or keep.shape != (n,) or not keep.is_contiguous():
+        raise RocketKVError(INVALID_ARG, f"keep: need {n} bytes or truth values, got {keep.dtype} {tuple(keep.shape)}")
+    _summaries(cache, kmax, kmin)
+    st, ch = cache.struct(), chunk.struct(cache)
+    here(cache, keep=keep, kmax=kmax, kmin=kmin, starts=chunk.starts, workspace=workspace)
+    if n == 0:
+        return
+    _check(call(C.byref(st), C.byref(ch), _ptr(keep), _ptr(kmax), _ptr(kmin), _ptr(workspace), workspace.numel(),
+                _stream(stream)))
+
+
+def keep_tokens(cache: Cache, chunk: Chunk, keep, kmax, kmin, workspace, stream=None):
+    """Of the chunk appended last, the tokens with keep != 0 (uint8 or bool [n_tokens]) stay; see rocketkv_keep_tokens."""
+    _keep(lib().rocketkv_keep_tokens, _here_with, cache, chunk, keep, kmax, kmin, workspace, stream)
+
+
+def q_keep_tokens(cache: QCache, chunk: Chunk, keep, kmax, kmin, workspace, stream=None):
+    """keep_tokens on a quantised cache."""
+    _keep(lib().rocketkv_q_keep_tokens, _here_with_q, cache, chunk, keep, kmax, kmin, workspace, stream)
 
 
 def decompose(seq_len: int, token_budget: int, head_dim: int = 128) -> dict:
