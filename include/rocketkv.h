@@ -477,7 +477,7 @@ int32_t rocketkv_weight_evict(const rocketkv_cache_t* src, const float* weights,
  * A block's power of two is the smallest with which none of its values exceeds the largest code (2^-100 at least, and at
  * most what keeps values in the range of bf16: 2^119 for E4M3, 2^125 for E2M1, beyond which codes are the largest); a value
  * becomes the nearest code, half way the even one.  A block that holds a value that is not finite becomes NaN as a whole,
- * scale 255; other scales lie in 27 .. 252.  Every value a code stands for is a bf16 value, so a quantised cache is exactly
+ * scale 255; other scales lie in 27 .. 246 (E4M3) or 27 .. 252 (E2M1).  Every value a code stands for is a bf16 value, so a quantised cache is exactly
  * the bf16 cache of those values in half or a quarter of the bytes, and what an operator computes on it is what its
  * counterpart computes on that cache.
  *

@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librocketkv.so")
 SOURCES = ["api.hip", "summaries.hip", "select.hip", "attend.hip", "attend_tok.hip", "decode.hip", "decode_tok.hip", "snapkv.hip", "probe.hip",
-           "rope.hip", "chunk_attend.hip", "weights.hip", "evict.hip", "q_attend.hip", "convert.hip", "tree.hip"]
+           "rope.hip", "chunk_attend.hip", "weights.hip", "evict.hip", "q_attend.hip", "q_attend_few.hip", "convert.hip", "tree.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Rpass-analysis=kernel-resource-usage",

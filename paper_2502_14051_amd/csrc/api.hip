@@ -1131,7 +1131,7 @@ size_t rocketkv_q_workspace_bytes(int32_t op, const rocketkv_qcache_t* cache, in
     case ROCKETKV_OP_ATTEND:
       if (a < 0) { fail(ROCKETKV_INVALID_ARG, "%s: pages_row_len must be >= 0", who); return 0; }
       if (check_list(cache, a, who)) return 0;
-      return plan_q_list(q_view_of(cache), a ? a : cache->pages_cap).total_bytes;
+      return plan_q_list(q_view_of(cache), a).total_bytes;
     case ROCKETKV_OP_HSA_DECODE:
       if (a < 1) { fail(ROCKETKV_INVALID_ARG, "%s: token_budget must be >= 1", who); return 0; }
       return plan_q_decode(cache, a).total;
@@ -1196,7 +1196,7 @@ int32_t rocketkv_q_chunk_attend(const rocketkv_qcache_t* cache, const rocketkv_c
   if (q == out) return fail(ROCKETKV_INVALID_ARG, "%s: q and out must be distinct", who);
   const QCacheView v = q_view_of(cache);
   const ChunkPlan plan = plan_q_attend(v, chunk->n_tokens);
-  if (plan.workgroups * 512 > 0xffffffffll) return fail(ROCKETKV_UNSUPPORTED, "%s: too many rows for one launch", who);
+  if (plan.workgroups * 1024 > 0xffffffffll) return fail(ROCKETKV_UNSUPPORTED, "%s: too many rows for one launch", who);
   if (int r = check_workspace(workspace, workspace_bytes, plan.total_bytes, who)) return r;
   const hipError_t e = launch_q_attend(v, chunk_of(chunk), mask ? MaskView{mask->bits, mask->words} : MaskView{nullptr, 0},
                                        static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out), out_lse, workspace, plan,
@@ -1217,7 +1217,7 @@ int32_t rocketkv_q_attend(const rocketkv_qcache_t* cache, const void* q, const i
   const int row_len = pages ? pages_row_len : cache->pages_cap;
   if (int r = check_list(cache, row_len, who)) return r;
   const QCacheView v = q_view_of(cache);
-  const ChunkPlan plan = plan_q_list(v, row_len);
+  const ChunkPlan plan = plan_q_list(v, pages ? row_len : 0);
   if (int r = check_workspace(workspace, workspace_bytes, plan.total_bytes, who)) return r;
   const hipError_t e = launch_q_list(v, pages, row_len, static_cast<const bf16_t*>(q), static_cast<bf16_t*>(out), out_lse,
                                      workspace, plan, static_cast<hipStream_t>(stream));

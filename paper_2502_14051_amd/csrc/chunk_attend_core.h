@@ -142,19 +142,11 @@ __device__ __forceinline__ void widen16(u32x2 raw, float scale, u32x4& lo, u32x4
   hi = eight(raw.y);
 #endif
 }
-// `scales`: of the four blocks of a token, `block`: which of them.  A block whose scale is 255 holds no numbers.
+// `scales`: of the four blocks of a token, `block`: which of them.  (The conversion takes the scale's exponent alone; the
+// highest, a scale byte of 255, gives NaN.)
 template <class Raw>
 __device__ __forceinline__ void widen16(Raw raw, uint32_t scales, int block, u32x4& lo, u32x4& hi) {
-  const uint32_t byte = (scales >> (8 * block)) & 0xffu;
-  widen16(raw, __uint_as_float(byte << 23), lo, hi);
-  if (__any(byte == 0xffu)) {
-    const uint32_t none = byte == 0xffu ? 0x7fc07fc0u : 0u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      lo[i] = none ? none : lo[i];
-      hi[i] = none ? none : hi[i];
-    }
-  }
+  widen16(raw, __uint_as_float(((scales >> (8 * block)) & 0xffu) << 23), lo, hi);
 }
 
 }  // namespace
@@ -171,6 +163,7 @@ struct ChunkAttendArgs {
   int mask_words;
   const int32_t* pages;      // kListed: [batch][KV heads][row_len]; null: every page
   int row_len;
+  int list_parts;
   const uint32_t *k_scales, *v_scales;  // of codes: a byte a block of 32 channels
   int tile_tokens;    // tokens of a row tile
   int slots, most;    // workgroups the chip holds at a time; parts at most
@@ -403,7 +396,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
   Found found = {-1, 0}, entry = {-1, 0};  // of the step to be requested next; kListed: the list's page for the one behind it
   uint32_t tok_at = 0;                     // where this lane's token of the step requested last lies, in tokens
   // (a lane's places are derived anew at each use: held over the loop they would take the registers that are left)
-  const auto piece_row = [&](int ln) { return first_tok + ln / 8; };
+  const auto piece_row = [&](uint32_t ln) { return (uint32_t)first_tok + ln / 8; };
   const int list_len = VIEW == kListed ? min(max(c.seq_lens[pl.b], 0), c.pages_cap * c.page_size) : 0;
   const auto list_entry = [&](int it) {  // (steps one after the other)
     const int t = it * kStep + lane;
@@ -432,8 +425,8 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
   const auto request = [&](const bf16_t* pool, const uint32_t* scales, Brought& to) {
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
-      const int ln = (int)use_late((uint32_t)lane);
-      const uint32_t at = (uint32_t)__shfl((int)tok_at, piece_row(ln) + 8 * p);
+      const uint32_t ln = use_late((uint32_t)lane);
+      const uint32_t at = (uint32_t)__shfl((int)tok_at, (int)(piece_row(ln) + 8 * p));
       const Raw* src = reinterpret_cast<const Raw*>(reinterpret_cast<const char*>(pool) + (uint64_t)at * kRowBytes) + ln % 8;
       to.codes[p] = STREAM ? __builtin_nontemporal_load(src) : *src;
       to.scales[p] = scales[at];
@@ -443,11 +436,11 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
   const auto put_keys = [&](auto to, const Brought& from) {
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
-      const int ln = (int)use_late((uint32_t)lane), r = piece_row(ln) + 8 * p;
+      const uint32_t ln = use_late((uint32_t)lane), r = piece_row(ln) + 8 * p;
       u32x4 lo, hi;
-      widen16(from.codes[p], from.scales[p], ln % 8 / 2, lo, hi);
+      widen16(from.codes[p], from.scales[p], (int)(ln % 8 / 2), lo, hi);
       unsigned char* at = s_tiles + decltype(to)::value * kKeyBytes + r * 256;
-      const int x = (2 * (ln % 8)) ^ (r & 15);
+      const uint32_t x = (2 * (ln % 8)) ^ (r & 15);
       *reinterpret_cast<u32x4*>(at + x * 16) = lo;
       *reinterpret_cast<u32x4*>(at + (x ^ 1) * 16) = hi;
     }
@@ -455,12 +448,12 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
   const auto put_values = [&](auto to, const Brought& from, unsigned long long valid) {
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
-      const int ln = (int)use_late((uint32_t)lane), r = piece_row(ln) + 8 * p;
+      const uint32_t ln = use_late((uint32_t)lane), r = piece_row(ln) + 8 * p;
       u32x4 lo, hi;
-      widen16(from.codes[p], from.scales[p], ln % 8 / 2, lo, hi);
+      widen16(from.codes[p], from.scales[p], (int)(ln % 8 / 2), lo, hi);
       if (valid != ~0ull && !(valid >> r & 1ull)) lo = hi = (u32x4){0u, 0u, 0u, 0u};  // (0 x NaN is not 0)
       unsigned char* at = s_tiles + (2 + decltype(to)::value) * kKeyBytes + r * 256;
-      const int x = (2 * (ln % 8)) ^ (4 * (r & 3));
+      const uint32_t x = (2 * (ln % 8)) ^ (4 * (r & 3));
       *reinterpret_cast<u32x4*>(at + x * 16) = lo;
       *reinterpret_cast<u32x4*>(at + (x ^ 1) * 16) = hi;
     }

@@ -407,6 +407,7 @@ struct ChunkPlan {
   bool cuts;        // keys may be divided
   int64_t workgroups;
   size_t total_bytes;
+  int list_parts;   // parts of every list of pages
 };
 ChunkPlan plan_chunk_attend(const CacheView& c, int n_tokens);
 // Which tokens of the chunk its rows see; null: those up to their own.
@@ -430,10 +431,15 @@ struct QCacheView {
   uint8_t *k_scales, *v_scales;
   int32_t format;    // rocketkv_q_format_t
 };
+// Attention of few rows: `tiles` of 16 rows a workgroup
+void plan_few(const CacheView& c, int n_tokens, int tiles, ChunkPlan& p);
+void plan_few_listed(const CacheView& c, int row_len, ChunkPlan& p);
+hipError_t launch_few_attend(const QCacheView& c, const ChunkAttendArgs& a, const ChunkPlan& plan, bool listed,
+                             uint32_t* counters, hipStream_t st);
 ChunkPlan plan_q_attend(const QCacheView& c, int n_tokens);
 hipError_t launch_q_attend(const QCacheView& c, const ChunkView& ch, const MaskView& mask, const bf16_t* q, bf16_t* out,
                            float* out_lse, void* ws, const ChunkPlan& plan, hipStream_t st);
-ChunkPlan plan_q_list(const QCacheView& c, int row_len);
+ChunkPlan plan_q_list(const QCacheView& c, int row_len);  // 0: no list, every page
 hipError_t launch_q_list(const QCacheView& c, const int32_t* pages, int row_len, const bf16_t* q, bf16_t* out, float* out_lse,
                          void* ws, const ChunkPlan& plan, hipStream_t st);
 hipError_t launch_q_append(const QCacheView& c, const ChunkView& ch, const RopeView& r, const int32_t* positions,

@@ -6,12 +6,25 @@
 
 namespace rkv {
 
+// Rows of a sequence on average up to which its keys are walked by wavefronts of their own.
+constexpr int kFewRows = 32;
+
 ChunkPlan plan_q_attend(const QCacheView& c, int n_tokens) {
   ChunkPlan p;
-  p.far = false;
-  p.stream = false;
+  p.far = p.stream = false;
   p.tile_rows = 256;
   plan_chunk_tiles(c.tokens, n_tokens, p);
+  const int64_t rows = (int64_t)n_tokens * c.tokens.group / c.tokens.batch;
+  if (rows <= kFewRows) plan_few(c.tokens, n_tokens, rows <= 16 ? 1 : 2, p);
+  return p;
+}
+
+ChunkPlan plan_q_list(const QCacheView& c, int row_len) {
+  ChunkPlan p;
+  p.tile_rows = 256;
+  plan_chunk_tiles(c.tokens, c.tokens.batch, p);  // (for the size of its workspace)
+  if (row_len > 0) plan_few_listed(c.tokens, row_len, p);
+  else plan_few(c.tokens, c.tokens.batch, 1, p);
   return p;
 }
 
@@ -20,37 +33,34 @@ template <Source SRC, View VIEW>
 void launch_q(const CacheView& c, const ChunkAttendArgs& a, const ChunkPlan& plan, hipStream_t st) {
   hipLaunchKernelGGL((chunk_attend_kernel<SRC, false, 8, false, VIEW>), dim3((unsigned)plan.workgroups), dim3(8 * kWave), 4 * kKeyBytes, st, c, a);
 }
-template <View VIEW>
-hipError_t launch_format(const QCacheView& c, ChunkAttendArgs a, const ChunkPlan& plan, hipStream_t st) {
+ChunkAttendArgs q_attend_args(const QCacheView& c, const ChunkView& ch, const bf16_t* q, bf16_t* out, float* out_lse, void* ws,
+                              const ChunkPlan& plan) {
+  ChunkAttendArgs a = chunk_attend_args(ch, q, out, out_lse, ws, plan);
   a.k_scales = reinterpret_cast<const uint32_t*>(c.k_scales);
   a.v_scales = reinterpret_cast<const uint32_t*>(c.v_scales);
-  if (c.format == ROCKETKV_Q_E4M3) launch_q<kE4M3, VIEW>(c.tokens, a, plan, st);
-  else launch_q<kE2M1, VIEW>(c.tokens, a, plan, st);
-  return launch_chunk_merge(c.tokens, a, plan, st);
+  return a;
 }
 }  // namespace
 
 hipError_t launch_q_attend(const QCacheView& c, const ChunkView& ch, const MaskView& mask, const bf16_t* q, bf16_t* out,
                            float* out_lse, void* ws, const ChunkPlan& plan, hipStream_t st) {
   if (ch.n_tokens == 0) return hipSuccess;
-  ChunkAttendArgs a = chunk_attend_args(ch, q, out, out_lse, ws, plan);
+  ChunkAttendArgs a = q_attend_args(c, ch, q, out, out_lse, ws, plan);
   a.mask = mask.bits;
   a.mask_words = mask.words;
-  return mask.bits ? launch_format<kMasked>(c, a, plan, st) : launch_format<kCausal>(c, a, plan, st);
-}
-
-ChunkPlan plan_q_list(const QCacheView& c, int row_len) {
-  QCacheView v = c;
-  v.tokens.pages_cap = row_len;
-  return plan_q_attend(v, c.tokens.batch);
+  if (plan.tile_rows < 256) return launch_few_attend(c, a, plan, false, static_cast<uint32_t*>(ws), st);
+  if (c.format == ROCKETKV_Q_E4M3) mask.bits ? launch_q<kE4M3, kMasked>(c.tokens, a, plan, st) : launch_q<kE4M3, kCausal>(c.tokens, a, plan, st);
+  else mask.bits ? launch_q<kE2M1, kMasked>(c.tokens, a, plan, st) : launch_q<kE2M1, kCausal>(c.tokens, a, plan, st);
+  return launch_chunk_merge(c.tokens, a, plan, st);
 }
 
 hipError_t launch_q_list(const QCacheView& c, const int32_t* pages, int row_len, const bf16_t* q, bf16_t* out,
                          float* out_lse, void* ws, const ChunkPlan& plan, hipStream_t st) {
-  ChunkAttendArgs a = chunk_attend_args({c.tokens.batch, nullptr}, q, out, out_lse, ws, plan);
+  ChunkAttendArgs a = q_attend_args(c, {c.tokens.batch, nullptr}, q, out, out_lse, ws, plan);
   a.pages = pages;
   a.row_len = row_len;
-  return launch_format<kListed>(c, a, plan, st);
+  a.list_parts = plan.list_parts;
+  return launch_few_attend(c, a, plan, true, static_cast<uint32_t*>(ws), st);
 }
 
 }  // namespace rkv

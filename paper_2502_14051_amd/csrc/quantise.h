@@ -62,7 +62,7 @@ __device__ __forceinline__ Codes8 quantise8(const float (&x)[8]) {
   return r;
 }
 
-// What eight codes stand for, in bf16, exactly.
+// What eight codes stand for, in bf16, exactly.  (The conversion takes the scale's exponent alone; the highest gives NaN.)
 template <int FMT>
 __device__ __forceinline__ uint4 restore8(uint2 codes, uint32_t scale) {
   uint4 v = make_uint4(0u, 0u, 0u, 0u);
@@ -80,7 +80,6 @@ __device__ __forceinline__ uint4 restore8(uint2 codes, uint32_t scale) {
     v.z = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes.x, s, 2));
     v.w = bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes.x, s, 3));
   }
-  if (scale == 255u) v = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
 #endif
   return v;
 }
