@@ -203,7 +203,7 @@ void append_chunk_kernel(CacheView c, AppendChunkArgs a) {
   float2* s_cs = reinterpret_cast<float2*>(s_mem);                                                    // [tokens][pairs]
   uint32_t* s_k = reinterpret_cast<uint32_t*>(s_mem + (size_t)kBlockTokens * kHeadDim / 2 * sizeof(float2));  // [tokens][64]
   uint32_t* s_v = s_k + kBlockTokens * kHeadDim / 2;
-  bf16_t* s_sum = reinterpret_cast<bf16_t*>(s_v + kBlockTokens * kHeadDim / 2);                        // [heads][2][128][pages]
+  bf16_t* s_sum = reinterpret_cast<bf16_t*>(FMT != kBf16 ? s_v : s_v + kBlockTokens * kHeadDim / 2);    // [heads][2][128][pages]
   const int tid = threadIdx.x, ps = c.page_size;
   const bool turns = a.rope.rot_dim > 0;
   const int span = a.pages * ps;  // token slots of a block of pages
@@ -382,6 +382,86 @@ void append_chunk_kernel(CacheView c, AppendChunkArgs a) {
   }
 }
 
+// Keys and values that come turned into a quantised cache: sixteen lanes take a page, token by token, eight channels each, so
+// the extremes of its keys stay in registers, and only they pass through LDS, a workgroup's pages next to each other.
+constexpr int kPutPages = kRopeT / kRowLanes;
+constexpr int kPutRows = 4;  // tokens a lane has requested at once
+
+template <int FMT>
+__global__ __launch_bounds__(kRopeT) void put_chunk_kernel(CacheView c, AppendChunkArgs a) {
+  __shared__ __align__(16) bf16_t s_sum[2 * kHeadDim * kPutPages];  // [extreme][channel][page]
+  const int tid = threadIdx.x, ps = c.page_size, span = kPutPages * ps, g = blockIdx.x % c.n_kv_heads;
+  const auto tiles = [&](int n) { return n > 0 ? (n + span - 2) / span + 1 : 0; };
+  int b, tile;
+  if (!locate_tile(c.batch, blockIdx.x / c.n_kv_heads, [&](int i) { return tiles(chunk_rows(a.ch, i)); }, b, tile)) return;
+  const NewTokens s = new_tokens(c, a.ch, b);
+  if (s.room) {
+    const int p0 = (s.old / span + tile) * kPutPages, p = p0 + tid / kRowLanes, lane16 = tid % kRowLanes;
+    const int lo = max(s.old, p * ps), hi = min(s.old + s.n, (p + 1) * ps);
+    const int64_t pp = lo < hi ? phys_page(c, b, p) : -1, tok = pp * c.stride_page + g * c.stride_head - p * ps;
+    const int64_t sums = (((int64_t)b * c.n_kv_heads + g) * kHeadDim + lane16 * 8) * c.pages_cap + p;
+    float mx[8], mn[8];
+    bool begun = lo % ps != 0 && lo < hi;  // by older tokens
+    if (a.kmax && begun)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mx[e] = bf16_to_f32(a.kmax[sums + e * c.pages_cap]), mn[e] = bf16_to_f32(a.kmin[sums + e * c.pages_cap]);
+    for (int t0 = lo; t0 < hi; t0 += kPutRows) {
+      uint4 k[kPutRows], v[kPutRows];
+#pragma unroll
+      for (int u = 0; u < kPutRows; ++u) {
+        const int64_t r = s.row + min(t0 + u, hi - 1) - s.old;
+        k[u] = ld16<true>(a.k + r * a.k_stride + g * kHeadDim + lane16 * 8);
+        v[u] = ld16<true>(a.v + r * a.v_stride + g * kHeadDim + lane16 * 8);
+      }
+#pragma unroll
+      for (int u = 0; u < kPutRows; ++u) {
+        if (t0 + u >= hi) break;
+        const Codes8 kc = quantise8<FMT>(unpack8(k[u]).x), vc = quantise8<FMT>(unpack8(v[u]).x);
+        if (pp >= 0) {
+          store_codes<FMT>(c.k_pool, a.k_scales, tok + t0 + u, lane16, kc);
+          store_codes<FMT>(c.v_pool, a.v_scales, tok + t0 + u, lane16, vc);
+        }
+        if (a.kmax) {
+          const Eight x = unpack8(restore8<FMT>(kc.codes, kc.scale));
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            if (!begun || x.x[e] > mx[e]) mx[e] = x.x[e];
+            if (!begun || x.x[e] < mn[e]) mn[e] = x.x[e];
+          }
+          begun = true;
+        }
+      }
+    }
+    if (a.kmax) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        bf16_t* to = s_sum + (lane16 * 8 + e) * kPutPages + tid / kRowLanes;
+        to[0] = (bf16_t)(__float_as_uint(mx[e]) >> 16);
+        to[kHeadDim * kPutPages] = (bf16_t)(__float_as_uint(mn[e]) >> 16);
+      }
+      __syncthreads();
+      const int first = max(s.old, p0 * ps) / ps - p0, last = (min(s.old + s.n, (p0 + kPutPages) * ps) - 1) / ps - p0;  // pages that took in a token
+      for (int i = tid; i < 2 * kHeadDim * (kPutPages / 8); i += kRopeT) {
+        const int pg = i % (kPutPages / 8) * 8, row = i / (kPutPages / 8);
+        bf16_t* out = (row / kHeadDim ? a.kmin : a.kmax) + (((int64_t)b * c.n_kv_heads + g) * kHeadDim + row % kHeadDim) * c.pages_cap + p0 + pg;
+        const bf16_t* in = s_sum + row * kPutPages + pg;
+        if (first <= pg && pg + 7 <= last) *reinterpret_cast<uint4*>(out) = *reinterpret_cast<const uint4*>(in);
+        else
+          for (int e = max(0, first - pg); e < 8 && pg + e <= last; ++e) out[e] = in[e];
+      }
+    }
+  }
+  // The last of a sequence's workgroups to have read its length stores the new one.
+  __syncthreads();
+  if (tid == 0 && s.room) {
+    uint32_t* n = a.arrived + read_slot(c, b);
+    if (__hip_atomic_fetch_add(n, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(tiles(s.n) * c.n_kv_heads) - 1) {
+      clear_reads(a.arrived, read_slot(c, b));
+      c.seq_lens[b] = s.old + s.n;
+    }
+  }
+}
+
 hipError_t launch_rope(const RopeView& r, const int32_t* positions, int n_tokens, int n_heads, const bf16_t* x,
                        int64_t x_stride, bf16_t* y, int64_t y_stride, hipStream_t st) {
   if (n_tokens == 0 || n_heads == 0) return hipSuccess;
@@ -416,6 +496,15 @@ hipError_t launch_append_any(const CacheView& c, uint8_t* k_scales, uint8_t* v_s
   a.q_out = q_out;
   a.kmax = kmax;
   a.kmin = kmin;
+  a.arrived = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + ROCKETKV_WS_HEADER_BYTES / 2);
+  if constexpr (FMT != kBf16) {
+    if (r.rot_dim == 0 && !q) {
+      const int64_t blocks = (int64_t)ch.n_tokens / (kPutPages * c.page_size) + 2ll * c.batch;
+      const int64_t tiles = blocks < ch.n_tokens ? blocks : ch.n_tokens;
+      hipLaunchKernelGGL(put_chunk_kernel<FMT>, dim3((unsigned)(tiles * c.n_kv_heads)), dim3(kRopeT), 0, st, c, a);
+      return hipGetLastError();
+    }
+  }
   // Blocks of about 128 tokens; smaller ones where there are few.
   int pages = ((128 + c.page_size - 1) / c.page_size + 7) / 8 * 8;
   if (pages > 32) pages = 32;  // 16 KiB of summaries a head
@@ -433,8 +522,7 @@ hipError_t launch_append_any(const CacheView& c, uint8_t* k_scales, uint8_t* v_s
   a.q_block = ch.n_tokens >= 32 * 2048 ? kBlockTokens : (ch.n_tokens + 2047) / 2048;
   const int64_t q_blocks = q ? (int64_t)ch.n_tokens / a.q_block + c.batch : 0;
   const int q_wgs = (int)(q_blocks < ch.n_tokens ? q_blocks : (q ? ch.n_tokens : 0));
-  a.arrived = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + ROCKETKV_WS_HEADER_BYTES / 2);
-  const size_t lds = (size_t)kBlockTokens * kHeadDim / 2 * sizeof(float2) + 2 * (size_t)kBlockTokens * kHeadDim * sizeof(bf16_t) +
+  const size_t lds = (size_t)kBlockTokens * kHeadDim / 2 * sizeof(float2) + (FMT == kBf16 ? 2 : 1) * (size_t)kBlockTokens * kHeadDim * sizeof(bf16_t) +
                      (kmax ? (size_t)a.heads_per_wg * 2 * kHeadDim * pages * sizeof(bf16_t) : 0);
   const int n_kv = a.kv_wgs * a.head_groups;
   const auto kernel = rope_is_odd(r) ? append_chunk_kernel<true, FMT> : append_chunk_kernel<false, FMT>;
