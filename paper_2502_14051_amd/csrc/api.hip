@@ -1071,6 +1071,8 @@ int check_mask(const uint32_t* bits, int32_t words, const char* who) {
 int check_list(const rocketkv_qcache_t* c, int32_t row_len, const char* who) {
   if ((int64_t)row_len * c->page_size > (int64_t)1 << 30)
     return fail(ROCKETKV_UNSUPPORTED, "%s: pages_row_len * page_size exceeds 2^30", who);
+  if (((int64_t)row_len * c->page_size + 31) / 32 * c->batch >= (int64_t)1 << 31)
+    return fail(ROCKETKV_UNSUPPORTED, "%s: batch * pages_row_len * page_size reaches 2^36", who);
   return ROCKETKV_OK;
 }
 
@@ -1130,10 +1132,14 @@ size_t rocketkv_q_workspace_bytes(int32_t op, const rocketkv_qcache_t* cache, in
       return op == ROCKETKV_OP_APPEND_CHUNK ? (size_t)ROCKETKV_WS_HEADER_BYTES : plan_q_attend(q_view_of(cache), a).total_bytes;
     case ROCKETKV_OP_ATTEND:
       if (a < 0) { fail(ROCKETKV_INVALID_ARG, "%s: pages_row_len must be >= 0", who); return 0; }
-      if (check_list(cache, a, who)) return 0;
+      if (check_list(cache, a ? a : cache->pages_cap, who)) return 0;
       return plan_q_list(q_view_of(cache), a).total_bytes;
     case ROCKETKV_OP_HSA_DECODE:
       if (a < 1) { fail(ROCKETKV_INVALID_ARG, "%s: token_budget must be >= 1", who); return 0; }
+      {
+        const rocketkv_cache_t part = common_part(cache);
+        if (check_list(cache, list_len_for_budget(&part, a), who)) return 0;
+      }
       return plan_q_decode(cache, a).total;
     default:
       fail(ROCKETKV_INVALID_ARG, "%s: unknown op %d", who, op);
@@ -1235,6 +1241,7 @@ int32_t rocketkv_q_hsa_decode(const rocketkv_qcache_t* cache, const void* q, con
   if (int r = check_select_args(&part, q, kmax, kmin, channel_budget, token_budget, n_recent_pages, who)) return r;
   if (int r = check_rows(out, (int64_t)cache->n_q_heads * kHeadDim, cache->n_q_heads, "out", who)) return r;
   if (q == out) return fail(ROCKETKV_INVALID_ARG, "%s: q and out must be distinct", who);
+  if (int r = check_list(cache, list_len_for_budget(&part, token_budget), who)) return r;
   const QDecodePlan d = plan_q_decode(cache, token_budget);
   if (int r = check_workspace(workspace, workspace_bytes, d.total, who)) return r;
   const QCacheView v = q_view_of(cache);

@@ -50,7 +50,8 @@ enum Source { kByChannel, kByToken, kE4M3, kE2M1 };  // bf16 by the layout of th
 enum View {
   kCausal,  // the tokens up to its own
   kMasked,  // those in front of the chunk, and of the chunk those its bits say
-  kListed   // one row per sequence: the tokens of a list of pages
+  kListed,  // one row per sequence: the tokens of a list of pages
+  kWhole    // one row per sequence: all of its tokens
 };
 
 constexpr int kStep = 64;                                        // keys per step
@@ -161,9 +162,8 @@ struct ChunkAttendArgs {
   int4* part_place;   // [workgroup] what the merge needs: first row in the packed tensors, rows and part, parts, ChunkPlace::next
   const uint32_t* mask;      // kMasked: [n_tokens][mask_words], bit j: the row sees token j of its chunk
   int mask_words;
-  const int32_t* pages;      // kListed: [batch][KV heads][row_len]; null: every page
+  const int32_t* pages;      // kListed: [batch][KV heads][row_len]
   int row_len;
-  int list_parts;
   const uint32_t *k_scales, *v_scales;  // of codes: a byte a block of 32 channels
   int tile_tokens;    // tokens of a row tile
   int slots, most;    // workgroups the chip holds at a time; parts at most
@@ -180,10 +180,9 @@ struct ChunkSeq {
 };
 template <View VIEW>
 __device__ __forceinline__ ChunkSeq chunk_seq(const CacheView& c, const ChunkAttendArgs& a, int b) {
-  if (VIEW == kListed && a.pages) return {b, 1, a.row_len * c.page_size};  // (the places of its list)
   ChunkSeq s = {b, 1, 0};
-  if (VIEW != kListed) s.row = chunk_first(a.ch, b);
-  if (VIEW != kListed) s.n = chunk_rows(a.ch, b);
+  if (VIEW != kWhole) s.row = chunk_first(a.ch, b);
+  if (VIEW != kWhole) s.n = chunk_rows(a.ch, b);
   const int cap = c.pages_cap * c.page_size, n = c.seq_lens[b];
   s.len = n < 0 ? 0 : (n > cap ? cap : n);
   return s;
@@ -393,24 +392,11 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
     Raw codes[kPieces];
     uint32_t scales[kPieces];
   };
-  Found found = {-1, 0}, entry = {-1, 0};  // of the step to be requested next; kListed: the list's page for the one behind it
+  Found found = {-1, 0};  // of the step to be requested next
   uint32_t tok_at = 0;                     // where this lane's token of the step requested last lies, in tokens
   // (a lane's places are derived anew at each use: held over the loop they would take the registers that are left)
   const auto piece_row = [&](uint32_t ln) { return (uint32_t)first_tok + ln / 8; };
-  const int list_len = VIEW == kListed ? min(max(c.seq_lens[pl.b], 0), c.pages_cap * c.page_size) : 0;
-  const auto list_entry = [&](int it) {  // (steps one after the other)
-    const int t = it * kStep + lane;
-    const Found e = {it >= it1 || t >= s.len ? -1 : a.pages ? a.pages[((int64_t)pl.b * c.n_kv_heads + g) * a.row_len + page] : page, slot};
-    slot += skip_slots;
-    page += skip_pages;
-    if (slot >= ps) { slot -= ps; ++page; }
-    return e;
-  };
-  const auto find = [&](int it, Found e) {
-    if (VIEW == kListed) {
-      const bool there = e.raw >= 0 && e.raw < c.pages_cap && e.raw * ps + e.slot < list_len;
-      return Found{there ? phys_page_request(c, pl.b, e.raw) : -1, e.slot};
-    }
+  const auto find = [&](int it) {  // (steps one after the other)
     const Found f = {it < it1 && it * kStep + lane < s.len ? phys_page_request(c, pl.b, page) : -1, slot};
     slot += skip_slots;
     page += skip_pages;
@@ -607,8 +593,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
       request(c.v_pool, a.v_scales, new_values);  // of it + 2 (behind the last step: from the pools' beginning, and unused)
       newest = locate(found);
       request(c.k_pool, a.k_scales, new_keys);  // of it + 3
-      found = find(it + 4, entry);
-      if (VIEW == kListed) entry = list_entry(it + 5);
+      found = find(it + 4);
     } else {
       off_v = off_k;
       issue_values(other);  // (behind the last step: from the pools' beginning, and unused)
@@ -663,15 +648,9 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
   if (it0 < it1) {
     if constexpr (CODES) {
       // the pages of the first steps beside each other, then all they bring
-      Found e[5], f[4];
-      if (VIEW == kListed)
+      Found f[4];
 #pragma unroll
-        for (int i = 0; i < 5; ++i) e[i] = list_entry(it0 + i);
-      else
-#pragma unroll
-        for (int i = 0; i < 5; ++i) e[i] = entry;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = find(it0 + i, e[i]);
+      for (int i = 0; i < 4; ++i) f[i] = find(it0 + i);
       Brought k0, v0, k1;
       valid0 = locate(f[0]);
       request(c.k_pool, a.k_scales, k0);
@@ -682,7 +661,6 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
       valid2 = locate(f[2]);
       request(c.k_pool, a.k_scales, new_keys);
       found = f[3];
-      entry = e[4];
       put_keys(std::integral_constant<int, 0>{}, k0);
       put_values(std::integral_constant<int, 0>{}, v0, valid0);
       put_keys(std::integral_constant<int, 1>{}, k1);

@@ -407,7 +407,6 @@ struct ChunkPlan {
   bool cuts;        // keys may be divided
   int64_t workgroups;
   size_t total_bytes;
-  int list_parts;   // parts of every list of pages
 };
 ChunkPlan plan_chunk_attend(const CacheView& c, int n_tokens);
 // Which tokens of the chunk its rows see; null: those up to their own.
@@ -432,10 +431,10 @@ struct QCacheView {
   int32_t format;    // rocketkv_q_format_t
 };
 // Attention of few rows: `tiles` of 16 rows a workgroup
+int64_t few_units_bound(const CacheView& c, int n_tokens, int tiles);  // units of all tiles, at most; below 2^31 for plan_few
 void plan_few(const CacheView& c, int n_tokens, int tiles, ChunkPlan& p);
-void plan_few_listed(const CacheView& c, int row_len, ChunkPlan& p);
-hipError_t launch_few_attend(const QCacheView& c, const ChunkAttendArgs& a, const ChunkPlan& plan, bool listed,
-                             uint32_t* counters, hipStream_t st);
+hipError_t launch_few_attend(const QCacheView& c, const ChunkAttendArgs& a, const ChunkPlan& plan, bool singles,
+                             uint32_t* counters, hipStream_t st);  // singles: a token per sequence, over its list of pages or all
 ChunkPlan plan_q_attend(const QCacheView& c, int n_tokens);
 hipError_t launch_q_attend(const QCacheView& c, const ChunkView& ch, const MaskView& mask, const bf16_t* q, bf16_t* out,
                            float* out_lse, void* ws, const ChunkPlan& plan, hipStream_t st);

@@ -2,10 +2,12 @@
 // so a host program can sweep it.
 //
 // A workgroup fills a compute unit; its wavefronts take units of 32 keys in turn, and a round of them takes as long as memory
-// does.  The keys of every tile of rows are cut into parts so that there are as many as compute units, but where a part
-// would be less than a round, and not where two rounds would do: handing results over takes about what a round takes.
-// (16 sequences' lists of 1024 tokens, 8 KV heads, us in one, two and four parts: 17.2, 18.8, 23.2; one sequence's of 2048
-// in one, two, four and eight: 19.4, 16.8, 14.7, 14.1.)
+// does.  The units of all tiles of a KV head stand in a row, tile behind tile, and every workgroup takes an equal piece of it,
+// wherever that begins and ends: lengths may differ as they like.  A tile that lies in several pieces has that many parts,
+// whose results are joined; of a piece only the first and the last tile can be such.
+// No piece is shorter than a round, and where tiles have two rounds at most they are whole as far as workgroups suffice:
+// handing results over takes about what a round takes.  (16 sequences' lists of 1024 tokens, 8 KV heads, us in one, two and
+// four parts: 17.2, 18.8, 23.2; one sequence's of 2048 in one, two, four and eight: 19.4, 16.8, 14.7, 14.1.)
 #pragma once
 #include <stdint.h>
 
@@ -17,27 +19,23 @@
 
 namespace rkv {
 
+constexpr int kFewMost = 256;  // pieces at most
 constexpr int kFewRound = 16;  // units that a workgroup's wavefronts take at a time
 
-// Parts of a tile that sees `units` units, at `share` parts to a unit.
-RKV_HD inline int few_parts(int units, float share) {
-  if (units <= 2 * kFewRound) return 1;
-  const int n = (int)((float)units * share), most = units / kFewRound;
-  return n < 1 ? 1 : n > most ? most : n;
+// Pieces of a row of `units` units of `tiles` tiles, `slots` at most.
+RKV_HD inline int few_pieces(int units, int tiles, int slots) {
+  const int n = units / 2 / kFewRound <= tiles && units <= 2 * kFewRound * (int64_t)tiles ? tiles : units / kFewRound;
+  return n > slots ? slots : n < 1 ? 1 : n;
 }
-
-// Parts to a unit.  `work`: units of all tiles, `tiles`: how many, `slots`: compute units; `count(share)`: parts of all tiles,
-// which the result keeps within `slots` unless the tiles alone exceed it.
-template <class Count>
-RKV_HD inline float few_share(float work, int tiles, int slots, const Count& count) {
-  if (tiles >= slots) return 0.f;
-  float share = (float)slots / work * 1.000001f;  // (so that equal tiles get what they should in spite of rounding)
-  for (int i = 0; i < 24; ++i) {
-    const int n = count(share);
-    if (n <= slots) return share;
-    share *= (float)slots / (float)n * 0.98f;
-  }
-  return 0.f;
+// First unit of piece k (of piece `pieces`: the end).  (Most rows are short enough for 32 bits, whose division is the shorter.)
+RKV_HD inline int few_begin(int units, int k, int pieces) {
+  if (units < (1 << 24)) return (int)((uint32_t)units * (uint32_t)k / (uint32_t)pieces);
+  return (int)((uint64_t)units * (uint64_t)k / (uint32_t)pieces);
+}
+// The piece that unit x lies in: the last that begins at x or before, begin(k) <= x being k < (x + 1) pieces / units.
+RKV_HD inline int few_piece_of(int units, int x, int pieces) {
+  if (units < (1 << 24)) return (int)(((uint32_t)(x + 1) * (uint32_t)pieces - 1u) / (uint32_t)units);
+  return (int)(((uint64_t)(x + 1) * (uint64_t)pieces - 1u) / (uint32_t)units);
 }
 
 }  // namespace rkv

@@ -21,7 +21,8 @@ namespace rkv {
 
 namespace {
 
-constexpr int few_waves(int tiles) { return tiles == 1 ? 16 : 8; }  // as many as registers allow
+constexpr int few_per_simd(int tiles) { return tiles == 1 ? 4 : tiles == 2 ? 3 : 2; }  // as many as registers allow
+constexpr int few_waves(int tiles) { return 4 * few_per_simd(tiles); }
 constexpr int kUnit = 32;                                       // keys a wavefront takes at a time
 constexpr int kUnitBytes = kUnit * kHeadDim * (int)sizeof(bf16_t);  // values of a unit, a tile's outputs
 
@@ -48,59 +49,83 @@ __device__ __forceinline__ f4 ld_agent4(float* base, uint32_t at) {
 #endif
 }
 
-// Where workgroup `at` of a KV head works, found by one wavefront.
+// The row of all tiles' units of a KV head, and the piece a workgroup takes.
+struct FewRow {
+  int units, pieces, from, to;
+};
+// The part of a tile that a piece holds, units u0 .. u1 - 1 of it.
+struct FewPart {
+  int b, row, n, len;       // the sequence, see ChunkSeq
+  int tile, u0, u1, end;    // end: of the part in the row
+  int part, parts, first;   // first: the piece that holds the tile's beginning
+};
+
 template <View VIEW>
-__device__ __forceinline__ bool few_place(const CacheView& c, const ChunkAttendArgs& a, int at, ChunkPlace& p, ChunkSeq& s) {
-  const int lane = threadIdx.x % kWave;
-  const ChunkSeq own = chunk_seq_of_lane<VIEW>(c, a);
-  const auto total = [](int x) { return __builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)x), kWave - 1); };
-  const auto tiles_of = [&](const ChunkSeq& s) { return VIEW == kListed ? 1 : chunk_ceil(s.n, a.tile_tokens); };
-  const auto each = [&](const auto& fn) {  // of the tiles and units of every sequence
+__device__ __forceinline__ int few_tiles(const ChunkAttendArgs& a, const ChunkSeq& s) {
+  return VIEW == kWhole ? 1 : chunk_ceil(s.n, a.tile_tokens);
+}
+__device__ __forceinline__ int few_units(const ChunkSeq& s) { return max(1, chunk_ceil(s.len, 32)); }  // (a tile without keys has one of none)
+
+// Both by one wavefront, a sequence a lane; `own`: of the first 64, looked up once.
+template <View VIEW>
+__device__ __forceinline__ FewRow few_row(const CacheView& c, const ChunkAttendArgs& a, const ChunkSeq& own, int at) {
+  int tiles = 0, units = 0;
+  if (VIEW == kListed) {
+    tiles = c.batch;
+    units = c.batch * max(1, chunk_ceil(a.row_len * c.page_size, 32));
+  } else {
+    const auto total = [](int x) { return __builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)x), kWave - 1); };
+    const int lane = threadIdx.x % kWave;
     for (int b0 = 0; b0 < c.batch; b0 += kWave) {
-      int t = 0, units = 0;
+      int t = 0, u = 0;
       if (b0 + lane < c.batch) {
         const ChunkSeq s = b0 == 0 ? own : chunk_seq<VIEW>(c, a, b0 + lane);
-        t = tiles_of(s);
-        units = t ? chunk_ceil(s.len, 32) : 0;
+        t = few_tiles<VIEW>(a, s);
+        u = few_units(s);
       }
-      fn(t, units);
+      tiles += total(t);
+      units += total(t * u);
     }
-  };
-  float share = 0.f;
-  if (a.partial) {
-    int tiles = 0;
-    float work = 0.f;
-    each([&](int t, int units) {
-      tiles += total(t) * c.n_kv_heads;
-      // (a coarser count keeps the sums in range where sequences are long: 2^16 units are 2^21 tokens)
-      work += (float)total(min(t, a.most) * min(units, 1 << 16)) * (float)c.n_kv_heads;
-    });
-    share = few_share(work, tiles, a.most, [&](float x) {
-      int n = 0;
-      each([&](int t, int units) { n += total(t * few_parts(units, x)); });
-      return n * c.n_kv_heads;
-    });
   }
-  int idx;
-  if (!locate_tile(c.batch, at, [&](int i) {
-        const ChunkSeq s = i < kWave ? own : chunk_seq<VIEW>(c, a, i);
-        return tiles_of(s) * few_parts(chunk_ceil(s.len, 32), share);
-      }, p.b, idx))
-    return false;
-  if (p.b < kWave) s = {__builtin_amdgcn_readlane(own.row, p.b), __builtin_amdgcn_readlane(own.n, p.b), __builtin_amdgcn_readlane(own.len, p.b)};
-  else s = chunk_seq<VIEW>(c, a, p.b);
-  p.parts = few_parts(chunk_ceil(s.len, 32), share);
-  p.next = tiles_of(s);
-  p.part = idx / p.next;
-  p.tile = p.next - 1 - idx % p.next;
-  p.first = at - p.part * p.next;
-  return true;
+  const int pieces = few_pieces(units, tiles, a.slots);
+  if (at >= pieces) return {units, pieces, 0, 0};
+  return {units, pieces, few_begin(units, at, pieces), few_begin(units, at + 1, pieces)};
+}
+template <View VIEW>
+__device__ __forceinline__ FewPart few_part(const CacheView& c, const ChunkAttendArgs& a, const ChunkSeq& own, const FewRow& r, int at, int from) {
+  FewPart p;
+  ChunkSeq s;
+  int idx, u;
+  if (VIEW == kListed) {
+    s = {0, 1, a.row_len * c.page_size};
+    u = few_units(s);
+    p.b = s.row = from / u;
+    idx = from - p.b * u;
+  } else {
+    locate_tile(c.batch, from, [&](int i) {
+      const ChunkSeq s = i < kWave ? own : chunk_seq<VIEW>(c, a, i);
+      return few_tiles<VIEW>(a, s) * few_units(s);
+    }, p.b, idx);
+    if (p.b < kWave) s = {__builtin_amdgcn_readlane(own.row, p.b), __builtin_amdgcn_readlane(own.n, p.b), __builtin_amdgcn_readlane(own.len, p.b)};
+    else s = chunk_seq<VIEW>(c, a, p.b);
+    u = few_units(s);
+  }
+  p.row = s.row, p.n = s.n, p.len = s.len;
+  p.tile = idx / u;
+  p.u0 = idx - p.tile * u;
+  const int begin = from - p.u0, end = begin + u;
+  p.end = min(r.to, end);
+  p.u1 = p.end - begin;
+  p.first = few_piece_of(r.units, begin, r.pieces);
+  p.part = at - p.first;
+  p.parts = few_piece_of(r.units, end - 1, r.pieces) - p.first + 1;
+  return p;
 }
 
 }  // namespace
 
 template <Source SRC, View VIEW, int NB>
-__global__ __launch_bounds__(few_waves(NB) * kWave) __attribute__((amdgpu_waves_per_eu(NB == 1 ? 4 : 2)))
+__global__ __launch_bounds__(few_waves(NB) * kWave) __attribute__((amdgpu_waves_per_eu(few_per_simd(NB))))
 void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
   constexpr int kRows = 16 * NB, kWaves = few_waves(NB);
   constexpr int kRowBytes = SRC == kE4M3 ? kHeadDim : kHeadDim / 2;
@@ -110,87 +135,104 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
   __shared__ float s_stats[kWaves][kRows][3];  // later [half a wavefront] of those that join parts
   __shared__ u32x4 s_q[NB * 4 * kWave];
   __shared__ int s_last;
-  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int i16 = lane % 16, kg = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int g = blockIdx.x % c.n_kv_heads, at = blockIdx.x / c.n_kv_heads;
-  // Lists are all of one length, which the host divides; sequences are divided here, by one wavefront for all.
-  ChunkPlace pl;
-  ChunkSeq s;
-  if (VIEW == kListed && a.pages) {
-    const int b = at % c.batch;
-    pl = {b, 0, at / c.batch, a.list_parts, b, c.batch};
-    s = {b, 1, a.row_len * c.page_size};
-  } else {
-    __shared__ ChunkPlace s_place;
-    __shared__ ChunkSeq s_seq;
-    if (wave == 0) {
-      if (!few_place<VIEW>(c, a, at, pl, s)) pl.parts = 0;
-      if (lane == 0) s_place = pl, s_seq = s;
-    }
-    __syncthreads();
-    const auto same = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
-    pl = {same(s_place.b), same(s_place.tile), same(s_place.part), same(s_place.parts), same(s_place.first), same(s_place.next)};
-    s = {same(s_seq.row), same(s_seq.n), same(s_seq.len)};
-    if (pl.parts == 0) return;
-  }
-  if (pl.parts > 1 && (int)blockIdx.x >= a.most) return;  // (`starts` that overlap)
+  __shared__ FewRow s_row;
+  __shared__ FewPart s_part;
   const int G = c.group, ps = c.page_size;
+  __shared__ ChunkSeq s_own[kWave];
+  const auto same = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  // (lists are all of one length, and take no looking up)
+  constexpr bool lists = VIEW == kListed;
+  FewRow whole = {0, 0, 0, 0};
+  if (lists) {
+    const FewRow r = few_row<VIEW>(c, a, {0, 0, 0}, at);
+    whole = {same(r.units), same(r.pieces), same(r.from), same(r.to)};
+  } else if (wave == 0) {
+    const int lane = threadIdx.x;
+    const ChunkSeq own = chunk_seq_of_lane<VIEW>(c, a);
+    s_own[lane] = own;
+    const FewRow r = few_row<VIEW>(c, a, own, at);
+    if (lane == 0) s_row = r;
+    if (r.from < r.to) {
+      const FewPart p = few_part<VIEW>(c, a, own, r, at, r.from);
+      if (lane == 0) s_part = p;
+    }
+  }
+  if (!lists) {
+    __syncthreads();
+    whole = {0, 0, same(s_row.from), same(s_row.to)};
+  }
+  const int to = whole.to;
+#pragma unroll 1
+  for (int from = whole.from; from < to;) {
+  // (a lane's places are derived anew at each use: held over the loops they would take the registers that are left)
+  const int tid = (int)use_late(threadIdx.x), lane = tid % kWave, i16 = lane % 16, kg = lane / 16;
+  if (lists) asm volatile("" : "+s"(whole.units));  // (nor the reciprocals that divide by it)
+  const FewPart found_part = lists ? few_part<VIEW>(c, a, {0, 0, 0}, whole, at, from) : s_part;
+  const FewPart pl = {same(found_part.b), same(found_part.row), same(found_part.n), same(found_part.len), same(found_part.tile),
+                      same(found_part.u0), same(found_part.u1), same(found_part.end), same(found_part.part),
+                      same(found_part.parts), same(found_part.first)};
+  const ChunkSeq s = {pl.row, pl.n, pl.len};
+  from = pl.end;
   const int t0 = pl.tile * a.tile_tokens, nt = min(a.tile_tokens, s.n - t0);
   const int rows = nt * G;
   const int old = s.len - s.n, pos0 = old + t0;
-
-  // the part's units
+  // its units that any row sees
   const int units = chunk_ceil(max(0, VIEW == kMasked ? s.len : min(s.len, pos0 + nt)), kUnit);
-  const int u0 = (int)((int64_t)units * pl.part / pl.parts), u1 = (int)((int64_t)units * (pl.part + 1) / pl.parts);
+  const int u0 = pl.u0, u1 = min(pl.u1, units);
 
   const auto packed_row = [&](int r) {  // (token, head) of the packed tensors
     const int t = r / G;
     return (int64_t)(s.row + t0 + t) * c.n_q_heads + (int64_t)g * G + (r - t * G);
   };
-  int last[NB];  // the last key each row sees
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    const int r = nb * 16 + i16;
-    last[nb] = r < rows ? pos0 + r / G : -1;
-  }
   // The queries as every wavefront's lanes read them (from LDS, unit after unit: registers are what there is little of).
-  for (int x = threadIdx.x; x < NB * 4 * kWave; x += kWaves * kWave) {
-    const int ln = x % kWave, j = x / kWave % 4, r = x / (4 * kWave) * 16 + ln % 16;
+  // Requested here, put there once the first unit is under way as well.
+  constexpr int kQueries = NB * 4 * kWave, kEach = (kQueries + kWaves * kWave - 1) / (kWaves * kWave);
+  u32x4 query[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int x = min(tid + i * kWaves * kWave, kQueries - 1), ln = x % kWave, j = x / kWave % 4, r = x / (4 * kWave) * 16 + ln % 16;
     const int channel = SRC == kE4M3 ? j / 2 * 64 + ln / 16 * 16 + j % 2 * 8 : ln / 16 * 32 + 8 * j;
-    u32x4 v = *reinterpret_cast<const u32x4*>(a.q + packed_row(min(r, rows - 1)) * kHeadDim + channel);
-    if (r >= rows) v = (u32x4){0u, 0u, 0u, 0u};
-    s_q[x] = v;
+    query[i] = *reinterpret_cast<const u32x4*>(a.q + packed_row(min(r, rows - 1)) * kHeadDim + channel);
+    if (r >= rows) query[i] = (u32x4){0u, 0u, 0u, 0u};
   }
+  const auto put_queries = [&]() {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (tid + i * kWaves * kWave < kQueries) s_q[tid + i * kWaves * kWave] = query[i];
+  };
+  if (kEach > 1) put_queries();  // (or at once, where that would take too many registers)
   const int sees_first = VIEW == kMasked ? old - 1 : pos0;  // the last key that all rows see
 
   // Where the tokens of a unit lie, lane i of the first 32 token i, looked up a unit ahead (and a list's pages two).
-  struct Found {
-    int raw, slot;
-  };
+  // (Its slot in the page is derived again when it is requested: a register less over the loop.)
   const int list_len = VIEW == kListed ? min(max(c.seq_lens[pl.b], 0), c.pages_cap * ps) : 0;
-  // (a lane's places are derived anew at each use: held over the loop they would take the registers that are left)
   const auto fresh = [&]() { return use_late((uint32_t)lane); };
+  const auto token = [&](int u) { return (uint32_t)(u * kUnit) + fresh() % kUnit; };
   const auto list_entry = [&](int u) {
-    const uint32_t t = (uint32_t)(u * kUnit) + fresh() % kUnit, p = t / (uint32_t)ps;
+    const uint32_t t = token(u), p = t / (uint32_t)ps;
     const int32_t* row = a.pages + ((int64_t)pl.b * c.n_kv_heads + g) * a.row_len;
-    return Found{u >= u1 || (int)t >= s.len ? -1 : a.pages ? row[p] : (int)p, (int)(t - p * ps)};
+    return u < u1 && (int)t < s.len ? row[p] : -1;
   };
-  const auto find = [&](int u, Found e) {
+  const auto find = [&](int u, int entry) {
+    const uint32_t t = token(u), p = t / (uint32_t)ps;
     if (VIEW == kListed) {
-      const bool there = e.raw >= 0 && e.raw < c.pages_cap && e.raw * ps + e.slot < list_len;
-      return Found{there ? phys_page_request(c, pl.b, e.raw) : -1, e.slot};
+      const bool there = entry >= 0 && entry < c.pages_cap && entry * ps + (int)(t - p * ps) < list_len;
+      return there ? phys_page_request(c, pl.b, entry) : -1;
     }
-    const uint32_t t = (uint32_t)(u * kUnit) + fresh() % kUnit, p = t / (uint32_t)ps;
-    return Found{u < u1 && (int)t < s.len ? phys_page_request(c, pl.b, (int)p) : -1, (int)(t - p * ps)};
+    return u < u1 && (int)t < s.len ? phys_page_request(c, pl.b, (int)p) : -1;
+  };
+  const auto in_range = [&](int raw) { return raw >= 0 && (int64_t)raw < c.n_phys_pages; };
+  const auto place_of = [&](int u, int raw) {  // counted in tokens over the pool; that of an absent one is the first
+    return in_range(raw) ? (uint32_t)(raw * c.stride_page + g * c.stride_head) + token(u) % (uint32_t)ps : 0u;
   };
 
   u32x4 k_raw[2][kKeyLoads];
   uint32_t k_scale[2], v_scale[4];
   Raw v_raw[4];
-  const auto request = [&](Found f) {  // returns a bit per token that exists
-    const bool there = f.raw >= 0 && (int64_t)f.raw < c.n_phys_pages;
-    const uint32_t tok = there ? (uint32_t)(f.raw * c.stride_page + g * c.stride_head + f.slot) : 0u;
-    const uint32_t valid = (uint32_t)__ballot(there);
+  const auto request = [&](int u, int raw) {  // returns a bit per token that exists
+    const uint32_t tok = place_of(u, raw), valid = (uint32_t)__ballot(in_range(raw));
     const uint8_t* vs = reinterpret_cast<const uint8_t*>(a.v_scales);
     const uint32_t ln = fresh();
 #pragma unroll
@@ -223,15 +265,17 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
 
   // Keys of row `nb * 16 + i16` among the 32 from key0 on, a bit each.
   const auto seen_bits = [&](int key0, int nb) -> uint32_t {
-    if (last[nb] < 0) return 0u;
+    const uint32_t r = nb * 16 + fresh() % 16;
+    if ((int)r >= rows) return 0u;
+    const uint32_t t = r / (uint32_t)G;
     if (VIEW != kMasked) {
-      const int n = last[nb] - key0 + 1;
+      const int n = pos0 + (int)t - key0 + 1;
       return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
     }
     const int j = key0 - old;
     if (j <= -32) return ~0u;
     const uint32_t* tile = a.mask + (int64_t)(s.row + t0) * a.mask_words;
-    const int w = j >> 5, place = (int)((nb * 16 + fresh() % 16) / (uint32_t)G) * a.mask_words + w;
+    const int w = j >> 5, place = (int)t * a.mask_words + w;
     const uint32_t lo = w < 0 ? ~0u : w < a.mask_words ? tile[place] : 0u, hi = w + 1 < a.mask_words ? tile[place + 1] : 0u;
     return (uint32_t)(((uint64_t)hi << 32 | lo) >> (j & 31));
   };
@@ -250,27 +294,32 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
   };
   int odd_from = -1;  // the first unit with a value that is no number among keys that not all rows see
   int u = u0 + wave;
-  Found entry = {-1, 0}, found = {-1, 0};
+  int entry = -1, found = -1;
   uint32_t valid = 0;
   if (u < u1) {
     if (VIEW == kListed) {
-      const Found e0 = list_entry(u), e1 = list_entry(u + kWaves);
+      const int e0 = list_entry(u), e1 = list_entry(u + kWaves);
       entry = list_entry(u + 2 * kWaves);
-      const Found f = find(u, e0);
+      const int f = find(u, e0);
       found = find(u + kWaves, e1);
-      valid = request(f);
+      valid = request(u, f);
     } else {
-      const Found f = find(u, entry);
+      const int f = find(u, entry);
       found = find(u + kWaves, entry);
-      valid = request(f);
+      valid = request(u, f);
     }
   }
+  if (kEach == 1) put_queries();
   __syncthreads();
+  if (!lists && wave == 0 && from < to) {  // (all have read where this part is)
+    const FewPart p = few_part<VIEW>(c, a, s_own[fresh()], s_row, at, from);
+    if (fresh() == 0) s_part = p;
+  }
   for (; u < u1; u += kWaves) {
     const int key0 = u * kUnit;
     const uint32_t there = valid;
     // values to LDS: chunk x of row r at x ^ 4 (r % 4)
-    const bool partly = there != ~0u || key0 + kUnit - 1 > sees_first, apart = VIEW != kListed && partly && rows > G;
+    const bool partly = there != ~0u || key0 + kUnit - 1 > sees_first, apart = !lists && partly && rows > G;
     bool odd = false;
     {
       const uint32_t ln = fresh();
@@ -280,19 +329,23 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
       for (int p = 0; p < 4; ++p) {
         u32x4 lo, hi;
         widen16(v_raw[p], __uint_as_float(v_scale[p] << 23), lo, hi);
-        if (partly) {
-          if (!(there >> (8 * p + ln / 8) & 1u)) lo = hi = (u32x4){0u, 0u, 0u, 0u};  // (0 x NaN is not 0)
-          if (apart) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t x = no_numbers(lo[e]), y = no_numbers(hi[e]);
-              lo[e] &= ~x, hi[e] &= ~y;
-              odd |= (x | y) != 0u;
-            }
-          }
-        }
         *reinterpret_cast<u32x4*>(s_tiles + (to + p * 2048)) = lo;
         *reinterpret_cast<u32x4*>(s_tiles + ((to ^ 16u) + p * 2048)) = hi;
+      }
+      if (partly) {
+#pragma unroll 1
+        for (uint32_t x = 0; x < 8; ++x) {  // (a lane's own pieces again)
+          u32x4* at = reinterpret_cast<u32x4*>(s_tiles + ((to ^ (x & 1u) * 16u) + x / 2 * 2048));
+          u32x4 v = *at;
+          const uint32_t live = there >> (x / 2 * 8 + ln / 8) & 1u ? ~0u : 0u;  // (0 x NaN is not 0)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t none = apart ? no_numbers(v[e]) & live : 0u;
+            v[e] &= live & ~none;
+            odd |= none != 0u;
+          }
+          *at = v;
+        }
       }
       if (apart && odd_from < 0 && __any(odd)) odd_from = u;
     }
@@ -317,15 +370,17 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
           S[nb][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kf[j]), as_bf16x8(queries[(nb * 4 + j) * kWave]), j == 0 ? (f4){0.f, 0.f, 0.f, 0.f} : S[nb][x], 0, 0, 0);
     }
     // what the next unit brings, while this one is worked on
-    if (u + kWaves < u1) {
-      valid = request(found);
+    const auto request_next = [&]() {
+      if (u + kWaves >= u1) return;
+      valid = request(u + kWaves, found);
       found = find(u + 2 * kWaves, entry);
       if (VIEW == kListed) entry = list_entry(u + 3 * kWaves);
-    }
+    };
+    if (NB < 4) request_next();
     u32x4 pf[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      if (partly || NB * 16 > rows) {
+      if (partly) {  // (rows that are not there see what they like)
         const uint32_t ok = (there & seen_bits(key0, nb)) >> (8 * kg);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -360,6 +415,7 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
       l[nb] += sum;
       lr[nb] += rounded;
     }
+    if (NB >= 4) request_next();  // (the logits' registers are free now, which their places in memory take)
     const uint32_t values_from = values_at();
 #pragma unroll
     for (int cb = 0; cb < 8; ++cb) {
@@ -371,15 +427,13 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
 
   // Values that are no numbers, of keys that not all rows see: where a row sees any in a channel, which a product of zeros and
   // ones says, its result is none either.
-  if (VIEW != kListed && odd_from >= 0) {
+  if (!lists && odd_from >= 0) {
 #pragma unroll 1
     for (u = odd_from; u < u1; u += kWaves) {
       const int key0 = u * kUnit;
       const uint32_t ln = fresh();
-      const Found f = find(u, entry);
-      const bool here = f.raw >= 0 && (int64_t)f.raw < c.n_phys_pages;
-      const uint32_t tok = here ? (uint32_t)(f.raw * c.stride_page + g * c.stride_head + f.slot) : 0u;
-      const uint32_t there = (uint32_t)__ballot(here);
+      const int raw = find(u, entry);
+      const uint32_t tok = place_of(u, raw), there = (uint32_t)__ballot(in_range(raw));
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
         const uint32_t r = 8 * p + ln / 8;
@@ -416,7 +470,10 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
   }
 
   // The wavefronts' results, a row tile at a time: four channels q of row i at place q ^ i, so that rows differ in banks.
-  const uint32_t part_row = (uint32_t)(at * c.n_kv_heads + g) * kRows;
+  const auto part_at = [&](int part) {  // a piece has places for the tile it ends with, if that goes on, and the one it goes on with
+    return (uint32_t)(((pl.first + part) * c.n_kv_heads + g) * 2 + (part == 0)) * kRows;
+  };
+  const uint32_t part_row = part_at(pl.part);
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     if (nb > 0) __syncthreads();
@@ -428,7 +485,7 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
 #pragma unroll
     for (int cb = 0; cb < 8; ++cb) *reinterpret_cast<f4*>(mine + i16 * 512 + ((4 * cb + kg) ^ i16) * 16) = O[nb][cb];
     __syncthreads();
-    for (int idx = threadIdx.x; idx < min(rows - nb * 16, 16) * 32; idx += kWaves * kWave) {
+    for (int idx = (int)use_late(threadIdx.x); idx < min(rows - nb * 16, 16) * 32; idx += kWaves * kWave) {
       const int i = idx / 32, q = idx % 32, r = nb * 16 + i;
       float M = kNegBig;
 #pragma unroll
@@ -460,21 +517,23 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
       }
     }
   }
-  if (pl.parts == 1) return;
+  if (pl.parts == 1) {
+    __syncthreads();  // (the next part's results come to the same places)
+    continue;
+  }
 
   // Whoever of the tile's workgroups is done last joins their results.  (See the hand-off of data between workgroups.)
   drain_stores();
   __syncthreads();
   uint32_t* counter = counters + pl.first * c.n_kv_heads + g;
-  if (threadIdx.x == 0)
+  if ((int)use_late(threadIdx.x) == 0)
     s_last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)pl.parts - 1;
   __syncthreads();
-  if (!s_last) return;
-  if (threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (!s_last) continue;
+  if ((int)use_late(threadIdx.x) == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   // 32 lanes a row, as many threads beside each other on its parts as there are to spare
   constexpr int kSlots = kWaves * 2;
-  const int share = max(1, kSlots / rows), slot = threadIdx.x / 32, q = threadIdx.x % 32;
-  const uint32_t row0 = (uint32_t)(pl.first * c.n_kv_heads + g) * kRows, next = (uint32_t)(pl.next * c.n_kv_heads) * kRows;
+  const int share = max(1, kSlots / rows), slot = (int)use_late(threadIdx.x) / 32, q = (int)use_late(threadIdx.x) % 32;
   for (int r0 = 0; r0 < rows; r0 += kSlots / share) {
     const int r = r0 + slot / share, first = slot % share;
     const bool works = r < rows && slot / share < kSlots / share;
@@ -488,7 +547,7 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
 #pragma unroll
         for (int x = 0; x < 4; ++x) {  // (absent ones weigh nothing, and read the first)
           const bool ok = p0 + x * share < pl.parts;
-          const uint32_t pr = row0 + (uint32_t)(ok ? p0 + x * share : p0) * next + r;
+          const uint32_t pr = part_at(ok ? p0 + x * share : p0) + r;
           const float* st = reinterpret_cast<const float*>(a.part_stats + pr);
           ms[x] = ld_agent(st), ss[x] = ld_agent(st + 1);
           v[x] = ld_agent4(a.partial, pr * kHeadDim + 4 * q);
@@ -537,31 +596,29 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
       if (a.out_lse && q == 0) a.out_lse[row] = sum == 0.f ? -INFINITY : (M + __log2f(sum)) * kLn2;
     }
   }
+  __syncthreads();  // (as above)
+  }
+}
+
+int64_t few_units_bound(const CacheView& c, int n_tokens, int tiles) {
+  const int tile_tokens = 16 * tiles / c.group;
+  const int64_t most_tiles = (int64_t)n_tokens / tile_tokens + c.batch;
+  return (most_tiles < n_tokens ? most_tiles : n_tokens) * (((int64_t)c.pages_cap * c.page_size + kUnit - 1) / kUnit);
 }
 
 void plan_few(const CacheView& c, int n_tokens, int tiles, ChunkPlan& p) {
   p.far = p.stream = false;
   p.tile_rows = 16 * tiles;
   p.tile_tokens = p.tile_rows / c.group;
-  p.slots = 256 * (16 / few_waves(tiles));
-  p.most = p.slots;
   int64_t most_tiles = (int64_t)n_tokens / p.tile_tokens + c.batch;
   if (most_tiles > n_tokens) most_tiles = n_tokens;
-  most_tiles *= c.n_kv_heads;
-  const int64_t at_least = ((int64_t)n_tokens + p.tile_tokens - 1) / p.tile_tokens * c.n_kv_heads;
-  // (where no sequence can be long enough to be cut, only the workgroups of tiles are launched)
-  p.cuts = at_least < p.most && (int64_t)c.pages_cap * c.page_size > 2 * kFewRound * kUnit;
-  p.workgroups = p.cuts && most_tiles < p.most ? p.most : most_tiles;
+  p.slots = few_pieces((int)few_units_bound(c, n_tokens, tiles), (int)most_tiles, c.n_kv_heads < kFewMost ? kFewMost / c.n_kv_heads : 1);
+  p.most = 2 * p.slots * c.n_kv_heads;
+  p.cuts = true;
+  p.workgroups = (int64_t)p.slots * c.n_kv_heads;
 }
 
-void plan_few_listed(const CacheView& c, int row_len, ChunkPlan& p) {
-  plan_few(c, c.batch, 1, p);
-  const int units = (int)(((int64_t)row_len * c.page_size + kUnit - 1) / kUnit), lists = c.batch * c.n_kv_heads;
-  p.list_parts = few_parts(units, few_share((float)lists * (float)units, lists, p.slots, [&](float x) { return lists * few_parts(units, x); }));
-  p.cuts = p.list_parts > 1;
-  p.workgroups = (int64_t)lists * p.list_parts;
-}
-
+namespace {
 template <View VIEW>
 hipError_t launch_few(const QCacheView& c, const ChunkAttendArgs& a, const ChunkPlan& plan, uint32_t* counters, hipStream_t st) {
   const int tiles = plan.tile_rows / 16;
@@ -570,14 +627,18 @@ hipError_t launch_few(const QCacheView& c, const ChunkAttendArgs& a, const Chunk
     return hipGetLastError();
   };
   const bool e4m3 = c.format == ROCKETKV_Q_E4M3;
-  if constexpr (VIEW != kListed)
-    if (plan.tile_rows == 32) return e4m3 ? launch(few_attend_kernel<kE4M3, VIEW, 2>) : launch(few_attend_kernel<kE2M1, VIEW, 2>);
+  if constexpr (VIEW == kCausal || VIEW == kMasked) {
+    if (tiles == 4) return e4m3 ? launch(few_attend_kernel<kE4M3, VIEW, 4>) : launch(few_attend_kernel<kE2M1, VIEW, 4>);
+    if (tiles == 2) return e4m3 ? launch(few_attend_kernel<kE4M3, VIEW, 2>) : launch(few_attend_kernel<kE2M1, VIEW, 2>);
+  }
   return e4m3 ? launch(few_attend_kernel<kE4M3, VIEW, 1>) : launch(few_attend_kernel<kE2M1, VIEW, 1>);
 }
 
-hipError_t launch_few_attend(const QCacheView& c, const ChunkAttendArgs& a, const ChunkPlan& plan, bool listed, uint32_t* counters,
+}  // namespace
+
+hipError_t launch_few_attend(const QCacheView& c, const ChunkAttendArgs& a, const ChunkPlan& plan, bool singles, uint32_t* counters,
                              hipStream_t st) {
-  if (listed) return launch_few<kListed>(c, a, plan, counters, st);
+  if (singles) return a.pages ? launch_few<kListed>(c, a, plan, counters, st) : launch_few<kWhole>(c, a, plan, counters, st);
   return a.mask ? launch_few<kMasked>(c, a, plan, counters, st) : launch_few<kCausal>(c, a, plan, counters, st);
 }
 

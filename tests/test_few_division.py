@@ -1,5 +1,5 @@
-"""How the attention of few rows over a quantised cache is divided, swept on the CPU from the header the kernels include: no
-more parts than workgroups are launched, none shorter than a round, all units covered once."""
+"""How the attention of few rows over a quantised cache is divided, swept on the CPU from the header the kernels include: pieces
+that cover all units once and evenly, places for what they hand over."""
 import os
 import subprocess
 
@@ -13,51 +13,58 @@ using namespace rkv;
 static uint64_t state = 88172645463325252ull;
 static uint32_t rnd(uint32_t n) { state ^= state << 13; state ^= state >> 7; state ^= state << 17; return (uint32_t)(state % n); }
 int main() {
-  int bad = 0, cut = 0;
-  static int tiles[300], units[300];
-  for (int trial = 0; trial < 60000; ++trial) {
-    const int slots = trial & 1 ? 256 : 512, B = 1 + rnd(trial % 3 == 0 ? 300 : 8), heads = 1 + rnd(16);
-    const int most_tiles = 1 + rnd(trial % 5 == 0 ? 40 : 2), longest = 1 + rnd(trial % 4 == 0 ? 60000 : 600);
-    int all = 0;
-    float work = 0.f;
+  int bad = 0, cut = 0, crossing = 0;
+  static int tiles[300], units[300], begin[4000], end[4000];
+  for (int trial = 0; trial < 60000 && bad < 10; ++trial) {
+    const int slots = 1 + rnd(256), B = 1 + rnd(trial % 3 == 0 ? 300 : 8), most_tiles = 1 + rnd(trial % 5 == 0 ? 12 : 2);
+    const int longest = trial % 9 == 0 ? 1 << 21 : 1 + rnd(trial % 4 == 0 ? 60000 : 600);
+    int64_t all = 0, sum = 0;
+    int n = 0;
     for (int b = 0; b < B; ++b) {
       tiles[b] = trial % 11 == 0 ? 1 : rnd(most_tiles + 1);
-      units[b] = tiles[b] ? trial % 6 == 0 ? longest : rnd(longest + 1) : 0;
-      all += tiles[b] * heads;
-      work += (float)tiles[b] * (float)units[b] * (float)heads;
-    }
-    const auto count = [&](float share) {
-      int64_t n = 0;
-      for (int b = 0; b < B; ++b) n += (int64_t)tiles[b] * few_parts(units[b], share);
-      return (int)(n * heads);
-    };
-    const float share = few_share(work, all, slots, count);
-    const int n = count(share);
-    if (n > (all > slots ? all : slots)) { ++bad; printf("trial %d: %d parts, %d tiles\n", trial, n, all); }
-    if (all >= slots && n != all) { ++bad; printf("trial %d: cut without need\n", trial); }
-    cut += n > all;
-    for (int b = 0; b < B; ++b) {
-      const int parts = few_parts(units[b], share);
-      if (parts > 1 && units[b] / parts < kFewRound) { ++bad; printf("trial %d: %d units in %d parts\n", trial, units[b], parts); }
-      int at = 0;
-      for (int p = 0; p < parts; ++p) {
-        const int u0 = (int)((int64_t)units[b] * p / parts), u1 = (int)((int64_t)units[b] * (p + 1) / parts);
-        if (u0 != at || u1 < u0) { ++bad; printf("trial %d: a gap\n", trial); }
-        at = u1;
+      units[b] = trial % 6 == 0 ? longest : 1 + rnd(longest);
+      for (int t = 0; t < tiles[b]; ++t) {
+        begin[n] = (int)sum;
+        sum += units[b];
+        end[n++] = (int)sum;
+        if (sum >= 1ll << 31) break;
       }
-      if (at != units[b]) { ++bad; printf("trial %d: units left over\n", trial); }
+      if (sum >= 1ll << 31) break;
+      all += tiles[b];
     }
-    if (bad > 10) break;
+    if (sum >= 1ll << 31 || n == 0) continue;
+    const int U = (int)sum, pieces = few_pieces(U, (int)all, slots);
+    if (pieces < 1 || pieces > slots) { ++bad; printf("trial %d: %d pieces for %d\n", trial, pieces, slots); }
+    if (pieces > 1 && U / pieces < kFewRound && U > 2 * kFewRound * all) { ++bad; printf("trial %d: short pieces\n", trial); }
+    if (few_begin(U, 0, pieces) != 0 || few_begin(U, pieces, pieces) != U) { ++bad; printf("trial %d: ends\n", trial); }
+    for (int k = 0; k < pieces; ++k) {
+      const int x0 = few_begin(U, k, pieces), x1 = few_begin(U, k + 1, pieces);
+      if (x0 != (int)((int64_t)U * k / pieces)) { ++bad; printf("trial %d: piece %d begins at %d\n", trial, k, x0); }
+      if (x1 - x0 > U / pieces + 1 || x1 - x0 < U / pieces) { ++bad; printf("trial %d: uneven\n", trial); }
+      if (x1 > x0 && (few_piece_of(U, x0, pieces) != k || few_piece_of(U, x1 - 1, pieces) != k)) { ++bad; printf("trial %d: piece %d\n", trial, k); }
+    }
+    // a piece's places: at most one tile begins in it and goes on, at most one goes on in it
+    static int goes_on[300], went_on[300];
+    for (int k = 0; k < pieces; ++k) goes_on[k] = went_on[k] = 0;
+    for (int t = 0; t < n; ++t) {
+      const int f = few_piece_of(U, begin[t], pieces), l = few_piece_of(U, end[t] - 1, pieces);
+      if (l > f) {
+        ++cut;
+        ++goes_on[f];
+        for (int k = f + 1; k <= l; ++k) ++went_on[k];
+      } else if (f > 0 && begin[t] > few_begin(U, f, pieces)) ++crossing;
+    }
+    for (int k = 0; k < pieces; ++k)
+      if (goes_on[k] > 1 || went_on[k] > 1) { ++bad; printf("trial %d: piece %d has no place\n", trial, k); }
   }
-  // equal tiles of many units fill the chip as far as whole parts do
-  for (int t = 1; t < 256; ++t)
-    for (int u = 600; u < 20000; u += 777) {
-      const auto count = [&](float s) { return t * few_parts(u, s); };
-      const int n = count(few_share((float)t * (float)u, t, 256, count)), want = 256 / t < u / kFewRound ? 256 / t : u / kFewRound;
-      if (n != t * want) { ++bad; printf("%d tiles of %d units: %d parts\n", t, u, n); break; }
-    }
-  printf("%d cut\n", cut);
-  return bad != 0 || cut < 5000;
+  // equal tiles: as many pieces to each as fit, none across two
+  for (int t = 1; t <= 32; t *= 2) {
+    const int pieces = few_pieces(t * 129, t, 32);
+    for (int k = 0; k < 32; ++k)
+      if (pieces != (t == 1 ? 8 : t == 2 ? 16 : 32) || (t > 2 && few_begin(t * 129, k * 32 / t, pieces) % 129 && k * 32 / t < 32 && k < t)) { ++bad; printf("%d tiles: %d pieces\n", t, pieces); break; }
+  }
+  printf("%d cut, %d whole beside others\n", cut, crossing);
+  return bad != 0 || cut < 5000 || crossing < 5000;
 }
 """
 
