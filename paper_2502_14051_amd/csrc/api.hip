@@ -1168,6 +1168,7 @@ int32_t rocketkv_tree_mask(int32_t batch, const rocketkv_chunk_t* chunk, const i
   g_err[0] = 0;
   const char* who = "rocketkv_tree_mask";
   if (batch < 1) return fail(ROCKETKV_INVALID_ARG, "%s: batch must be positive", who);
+  if (batch >= ROCKETKV_MAX_CHUNK) return fail(ROCKETKV_UNSUPPORTED, "%s: batch %d exceeds %d", who, batch, ROCKETKV_MAX_CHUNK - 1);
   if (int r = check_chunk(chunk, who)) return r;
   if (!parents && chunk->n_tokens > 0) return fail(ROCKETKV_INVALID_ARG, "%s: parents must not be NULL", who);
   if (!base != !positions) return fail(ROCKETKV_INVALID_ARG, "%s: base and positions go together", who);

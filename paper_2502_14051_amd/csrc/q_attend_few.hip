@@ -614,7 +614,7 @@ void plan_few(const CacheView& c, int n_tokens, int tiles, ChunkPlan& p) {
   if (most_tiles > n_tokens) most_tiles = n_tokens;
   p.slots = few_pieces((int)few_units_bound(c, n_tokens, tiles), (int)most_tiles, c.n_kv_heads < kFewMost ? kFewMost / c.n_kv_heads : 1);
   p.most = 2 * p.slots * c.n_kv_heads;
-  p.cuts = true;
+  p.cuts = p.slots > 1;
   p.workgroups = (int64_t)p.slots * c.n_kv_heads;
 }
 

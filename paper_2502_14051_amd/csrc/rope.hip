@@ -500,9 +500,11 @@ hipError_t launch_append_any(const CacheView& c, uint8_t* k_scales, uint8_t* v_s
   if constexpr (FMT != kBf16) {
     if (r.rot_dim == 0 && !q) {
       const int64_t blocks = (int64_t)ch.n_tokens / (kPutPages * c.page_size) + 2ll * c.batch;
-      const int64_t tiles = blocks < ch.n_tokens ? blocks : ch.n_tokens;
-      hipLaunchKernelGGL(put_chunk_kernel<FMT>, dim3((unsigned)(tiles * c.n_kv_heads)), dim3(kRopeT), 0, st, c, a);
-      return hipGetLastError();
+      const int64_t wgs = (blocks < ch.n_tokens ? blocks : ch.n_tokens) * c.n_kv_heads;
+      if (wgs * kRopeT <= 0xffffffffll) {  // (what a grid may have)
+        hipLaunchKernelGGL(put_chunk_kernel<FMT>, dim3((unsigned)wgs), dim3(kRopeT), 0, st, c, a);
+        return hipGetLastError();
+      }
     }
   }
   // Blocks of about 128 tokens; smaller ones where there are few.

@@ -709,20 +709,27 @@ class QCache:
     format: int = Q_E4M3
 
     def struct(self) -> QCacheStruct:
+        k, v, ks, vs, table = self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.block_table
         width = q_row_bytes(self.format)
-        stride_page, stride_head = self.k_scales.stride()[:2]
+        shape, strides = ks.shape, ks.stride()
+        page, head = strides[0] // 4, strides[1] // 4  # in tokens
+        rows, at = shape[:3] + (width,), (page * width, head * width, width, 1)
+        if (shape[1:] != (self.n_kv_heads, self.page_size, 4) or strides[2:] != (4, 1) or k.shape != rows or v.shape != rows or
+                vs.shape != shape or k.stride() != at or v.stride() != at or vs.stride() != strides or
+                k.element_size() + v.element_size() + ks.element_size() + vs.element_size() != 4):
+            self._refuse(width)
+        return QCacheStruct(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_size, self.pages_cap,
+                            shape[0], page, head, self.seq_lens.data_ptr(), None if table is None else table.data_ptr(),
+                            k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), self.format)
+
+    def _refuse(self, width):
+        """Says which of the tensors is none a cache can have."""
         shape = (self.k_codes.shape[0], self.n_kv_heads, self.page_size)
         for name, t, w in (("k_codes", self.k_codes, width), ("v_codes", self.v_codes, width), ("k_scales", self.k_scales, 4),
                            ("v_scales", self.v_scales, 4)):
             if t.element_size() != 1 or t.shape != shape + (w,):
                 raise RocketKVError(INVALID_ARG, f"{name}: need bytes {shape + (w,)}, got {t.dtype} {tuple(t.shape)}")
-            if t.stride() != (stride_page // 4 * w, stride_head // 4 * w, w, 1):
-                raise RocketKVError(INVALID_ARG, f"{name}: strides must be those of k_scales in tokens, rows contiguous")
-        table = self.block_table
-        return QCacheStruct(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_size, self.pages_cap,
-                            shape[0], stride_page // 4, stride_head // 4, _ptr(self.seq_lens),
-                            None if table is None else table.data_ptr(), self.k_codes.data_ptr(), self.v_codes.data_ptr(),
-                            self.k_scales.data_ptr(), self.v_scales.data_ptr(), self.format)
+        raise RocketKVError(INVALID_ARG, "strides of codes and scales must be the same in tokens, rows contiguous")
 
 
 def q_row_bytes(format: int) -> int:

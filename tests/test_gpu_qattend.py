@@ -70,6 +70,20 @@ def test_tiles_beside_the_chip(fmt, news, lens):
 
 
 @pytest.mark.parametrize("fmt", qr.FORMATS)
+@pytest.mark.parametrize("hq,hkv", [(8, 2), (3, 1), (16, 1), (40, 8)])
+@pytest.mark.parametrize("lens,news", [
+    ([60] * 5 + [300], [1] * 5 + [60]),          # single tokens, and a sequence of many tiles among them
+    ([5000, 3000, 17, 900], [4, 3, 2, 1]),        # pieces that end inside one tile and go on in the next
+    ([2000, 0, 33, 7000, 1], [8, 0, 7, 1, 1]),
+    ([40000, 64], [1, 1]), ([33] * 70, [1] * 70), ([600] * 40, [2] * 40),
+])
+def test_few_rows(fmt, hq, hkv, lens, news):
+    """Wavefronts with keys of their own: tiles of 16, 32 and 64 rows, cut where the pieces of the work end."""
+    c = ref.Case(8, lens, news, hq, hkv, 16, True)
+    ref.check_attention(c, *attend(c, qr.take_over(c, fmt, 8)))
+
+
+@pytest.mark.parametrize("fmt", qr.FORMATS)
 def test_one_workspace_for_all(fmt):
     ws = None
     for lens, news in (([9000], [70]), ([40], [40]), ([9000, 9000], [1, 300]), ([5000], [3]), ([5000], [1])):
@@ -152,7 +166,8 @@ CACHES = [(None, 16, False), (None, 16, True), (None, 3, True), (rk.Q_E4M3, 16, 
 
 @pytest.mark.parametrize("fmt,ps,token_major", CACHES)
 @pytest.mark.parametrize("kind", ["tree", "random", "none", "all"])
-@pytest.mark.parametrize("lens,news", [([1], [1]), ([40], [40]), ([300, 64, 33, 129], [33, 64, 1, 32]), ([130, 700], [70, 300]), ([5000, 9000], [12, 6])])
+@pytest.mark.parametrize("lens,news", [([1], [1]), ([40], [40]), ([300, 64, 33, 129], [33, 64, 1, 32]), ([130, 700], [70, 300]), ([5000, 9000], [12, 6]),
+                                       ([300, 8, 77], [5, 3, 4]), ([90, 3000], [8, 7]), ([200, 1, 40, 33], [1, 1, 40, 1])])
 def test_masks(fmt, ps, token_major, kind, lens, news):
     c = ref.Case(31, lens, news, 8, 2, ps if fmt is None else 16, token_major, pad=(2, 1))
     q = c.cache if fmt is None else qr.take_over(c, fmt, ps)
@@ -373,7 +388,7 @@ def test_a_tree_verified_step_by_step(fmt):
 
     warm = state()
     step(warm)
-    eager, captured = state(), state()
+    eager, captured, alone = state(), state(), state()
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
@@ -396,8 +411,20 @@ def test_a_tree_verified_step_by_step(fmt):
         assert captured["cache"].seq_lens.tolist() == total
         for x, y in zip(everything(captured), everything(eager)):
             assert torch.equal(x, y)
-    # the path's tokens stand behind each other, at the positions they were turned for: as if they had been appended alone
-    assert (eager["out"].float().abs().amax() < 100) and torch.isfinite(eager["lse"]).all()
+        # the paths' tokens stand behind each other, at the positions they were turned for: as if they alone had been appended
+        rows = [r for r in range(B * n) if flags.flatten()[r]]
+        few = rk.Chunk(torch.tensor([0, int(flags[0].sum()), len(rows)], dtype=torch.int32).cuda(), len(rows))
+        (rk.append_chunk if fmt is None else rk.q_append_chunk)(alone["cache"], few, static["k"][rows], static["v"][rows], alone["kmax"],
+                                                                 alone["kmin"], alone["wsa"], rope=rope)
+        for b in range(B):
+            if fmt is None:
+                got, want = ([x[b, :, :total[b]] for x in rk.unpack_cache(s["cache"])] for s in (eager, alone))
+                assert all(torch.equal(x, y) for x, y in zip(got, want))
+            else:
+                assert all((x == y).all() for x, y in zip(qr.tokens(eager["cache"], b, total[b]), qr.tokens(alone["cache"], b, total[b])))
+            at = slice(lens[b] // ps + 1, (total[b] + ps - 1) // ps)  # (the pages before hold older keys, whose summaries nobody made)
+            assert torch.equal(eager["kmax"][b, :, :, at], alone["kmax"][b, :, :, at])
+    assert torch.isfinite(eager["lse"]).all()
 
 
 @pytest.mark.parametrize("fmt", qr.FORMATS)
@@ -425,3 +452,65 @@ def test_two_graphs_one_workspace_and_another_stream(fmt):
         assert torch.equal(outs[i][0], want[i][0]) and torch.equal(outs[i][1], want[i][1])
     for c, (out, lse) in zip(cases, outs):
         ref.check_attention(c, out, lse)
+
+
+def far_cache(c, fmt, ps=64):
+    """The Case's tokens in a quantised cache whose rows lie beyond 4 GiB of codes, pages and heads at strides of their own."""
+    per = (max(c.lens) + 40) // ps + 2
+    per = (per + 7) // 8 * 8
+    width = rk.q_row_bytes(fmt)
+    n_phys = (5 << 30) // (c.hkv + 1) // ps // width
+    mk = lambda w: torch.empty((n_phys, c.hkv + 1, ps, w), dtype=torch.uint8, device="cuda")[:, 1:]
+    table = (n_phys - 1 - torch.arange(len(c.lens) * per)).reshape(len(c.lens), per).to(torch.int32).cuda()
+    return rk.QCache(len(c.lens), c.hq, c.hkv, 128, ps, per, mk(width), mk(width), mk(4), mk(4),
+                     torch.zeros((len(c.lens),), dtype=torch.int32, device="cuda"), table, fmt)
+
+
+@pytest.mark.parametrize("fmt", qr.FORMATS)
+def test_codes_beyond_4_gib(fmt):
+    """Offsets that take more than 32 bits: conversion there and back, append, attention of few and many rows, keeping."""
+    lens = [500, 300]
+    c = ref.Case(71, lens, [1, 2], 8, 2, 16, True)
+    q = far_cache(c, fmt)
+    rk.quantise(c.cache, q)
+    near = qr.take_over(c, fmt)
+    back = rk.alloc_cache(2, 8, 2, 128, 16, 40, "cuda", v_layout=rk.V_TOKEN_MAJOR)
+    rk.restore(q, back)
+    k, v = rk.unpack_cache(back)
+    for b, n in enumerate(lens):
+        assert torch.equal(k[b, :, :n], c.K[b, :, :n]) and torch.equal(v[b, :, :n], c.V[b, :, :n])
+        for got, want in zip(qr.tokens(q, b, n), qr.tokens(near, b, n)):
+            assert (got == want).all()
+    ref.check_attention(c, *attend(c, q))
+    new = torch.randn((40, 2, 128), generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).cuda()
+    chunk = rk.Chunk(torch.tensor([0, 30, 40], dtype=torch.int32).cuda(), 40)
+    ws = rk.q_alloc_workspace(rk.OP_APPEND_CHUNK, q, 40)
+    for cache in (q, near):
+        if cache is near:
+            near = cache = qr.like(c.cache, fmt, 16, spare=8)
+            rk.quantise(c.cache, cache)
+        rk.q_append_chunk(cache, chunk, new, new, None, None, ws)
+    qs = torch.randn((40, 8, 128), generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).cuda()
+    outs = []
+    for cache in (q, near):
+        out, lse = torch.empty_like(qs), torch.empty((40, 8), device="cuda")
+        rk.q_chunk_attend(cache, chunk, qs, out, lse, rk.q_alloc_workspace(rk.OP_CHUNK_ATTEND, cache, 40))
+        keep = (torch.arange(40) % 3 == 0).cuda()
+        rk.q_keep_tokens(cache, chunk, keep, None, None, ws)
+        outs.append((out, lse, cache.seq_lens.clone()) + tuple(torch.from_numpy(x) for b, n in enumerate((510, 304)) for x in qr.tokens(cache, b, n)))
+    for x, y in zip(*outs):
+        assert torch.equal(x, y)
+
+
+def test_masked_beyond_4_gib():
+    """The form for pools whose rows take more than 32 bits of offset, with a mask."""
+    lens, news = [700, 90], [40, 12]
+    c = ref.Case(72, lens, news, 8, 2, 16, True, shuffled=False)
+    per, n_phys = c.cache.pages_cap, (5 << 30) // (2 * 16 * 256)
+    pools = [torch.empty((n_phys, 2, 16, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for pool, old in zip(pools, (c.cache.k_pool, c.cache.v_pool)):
+        pool[-2 * per:] = old[:2 * per]
+    table = (n_phys - 2 * per + torch.arange(2 * per)).reshape(2, per).to(torch.int32).cuda()
+    far = rk.Cache(2, 8, 2, 128, 16, per, pools[0], pools[1], c.cache.seq_lens, table, rk.V_TOKEN_MAJOR)
+    m = qr.MaskedCase(c, masked(5, lens, news, "tree"))
+    m.check(*attend(c, far, m.mask))

@@ -133,11 +133,12 @@ def test_masked_attend_needs_a_mask_and_a_cache(L):
 @pytest.mark.parametrize("kw,status,needle", [
     (dict(q=Q + 8), rk.INVALID_ARG, "q must be"), (dict(out=None), rk.INVALID_ARG, "out must not"), (dict(out=Q), rk.INVALID_ARG, "distinct"),
     (dict(row=0), rk.INVALID_ARG, "pages_row_len"), (dict(row=1 << 27), rk.UNSUPPORTED, "2^30"),
+    (dict(row=1 << 26, batch=512, n_phys_pages=512 * 256), rk.UNSUPPORTED, "2^36"),
     (dict(ws=None), rk.WORKSPACE_TOO_SMALL, "workspace"), (dict(wsb=1000), rk.WORKSPACE_TOO_SMALL, "workspace"), (dict(ws=WS + 8), rk.INVALID_ARG, "aligned"),
 ])
 def test_listed_refusals(L, kw, status, needle):
-    a = dict(dict(q=Q, pages=LIST, row=64, out=OUT, ws=WS, wsb=BIG), **kw)
-    refused(L.rocketkv_q_attend(by(qcache()), a["q"], a["pages"], a["row"], a["out"], LSE, a["ws"], a["wsb"], None), status, needle)
+    a = dict(dict(q=Q, pages=LIST, row=64, out=OUT, ws=WS, wsb=BIG, batch=2, n_phys_pages=512), **kw)
+    refused(L.rocketkv_q_attend(by(qcache(batch=a["batch"], n_phys_pages=a["n_phys_pages"])), a["q"], a["pages"], a["row"], a["out"], LSE, a["ws"], a["wsb"], None), status, needle)
 
 
 @pytest.mark.parametrize("kw,status,needle", [
@@ -183,6 +184,7 @@ def test_keep_refusals(L, kw, status, needle):
     (dict(batch=0), rk.INVALID_ARG, "batch"), (dict(chunk=None), rk.INVALID_ARG, "chunk is NULL"), (dict(parents=None), rk.INVALID_ARG, "parents"),
     (dict(base=None), rk.INVALID_ARG, "go together"), (dict(pos=None), rk.INVALID_ARG, "go together"), (dict(bits=None), rk.INVALID_ARG, "bits"),
     (dict(words=0), rk.INVALID_ARG, "words"), (dict(chunk=chunk(n_tokens=rk.MAX_CHUNK + 1)), rk.UNSUPPORTED, "n_tokens"),
+    (dict(batch=rk.MAX_CHUNK), rk.UNSUPPORTED, "batch"),
 ])
 def test_tree_mask_refusals(L, kw, status, needle):
     a = dict(dict(batch=2, chunk=chunk(), parents=PARENTS, base=LIST, bits=BITS, words=1, pos=POS), **kw)
