@@ -38,4 +38,17 @@ RKV_HD inline int few_piece_of(int units, int x, int pieces) {
   return (int)(((uint64_t)(x + 1) * (uint64_t)pieces - 1u) / (uint32_t)units);
 }
 
+// Division of numbers below 2^31 by the same one again and again: n / d = (hi(n m) + n) >> l with l = ceil(log2 d) and
+// m = floor(2^32 (2^l - d) / d) + 1 (Granlund and Montgomery 1994).
+struct Divider {
+  uint32_t m;
+  int32_t l;
+};
+inline Divider divider(int d) {
+  int l = 0;
+  while ((1 << l) < d) ++l;
+  return {(uint32_t)(((((uint64_t)1 << l) - (uint64_t)d) << 32) / (uint64_t)d + 1u), l};
+}
+RKV_HD inline uint32_t divide(uint32_t n, Divider by) { return ((uint32_t)(((uint64_t)n * by.m) >> 32) + n) >> by.l; }
+
 }  // namespace rkv

@@ -126,7 +126,7 @@ __device__ __forceinline__ FewPart few_part(const CacheView& c, const ChunkAtten
 
 template <Source SRC, View VIEW, int NB>
 __global__ __launch_bounds__(few_waves(NB) * kWave) __attribute__((amdgpu_waves_per_eu(few_per_simd(NB))))
-void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
+void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters, Divider by_page) {
   constexpr int kRows = 16 * NB, kWaves = few_waves(NB);
   constexpr int kRowBytes = SRC == kE4M3 ? kHeadDim : kHeadDim / 2;
   constexpr int kKeyLoads = SRC == kE4M3 ? 2 : 1;  // of 16 bytes, a lane's 32 codes of a key
@@ -211,12 +211,12 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
   const auto fresh = [&]() { return use_late((uint32_t)lane); };
   const auto token = [&](int u) { return (uint32_t)(u * kUnit) + fresh() % kUnit; };
   const auto list_entry = [&](int u) {
-    const uint32_t t = token(u), p = t / (uint32_t)ps;
+    const uint32_t t = token(u), p = divide(t, by_page);
     const int32_t* row = a.pages + ((int64_t)pl.b * c.n_kv_heads + g) * a.row_len;
     return u < u1 && (int)t < s.len ? row[p] : -1;
   };
   const auto find = [&](int u, int entry) {
-    const uint32_t t = token(u), p = t / (uint32_t)ps;
+    const uint32_t t = token(u), p = divide(t, by_page);
     if (VIEW == kListed) {
       const bool there = entry >= 0 && entry < c.pages_cap && entry * ps + (int)(t - p * ps) < list_len;
       return there ? phys_page_request(c, pl.b, entry) : -1;
@@ -225,7 +225,8 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters) {
   };
   const auto in_range = [&](int raw) { return raw >= 0 && (int64_t)raw < c.n_phys_pages; };
   const auto place_of = [&](int u, int raw) {  // counted in tokens over the pool; that of an absent one is the first
-    return in_range(raw) ? (uint32_t)(raw * c.stride_page + g * c.stride_head) + token(u) % (uint32_t)ps : 0u;
+    const uint32_t t = token(u), slot = t - divide(t, by_page) * (uint32_t)ps;
+    return in_range(raw) ? (uint32_t)(raw * c.stride_page + g * c.stride_head) + slot : 0u;
   };
 
   u32x4 k_raw[2][kKeyLoads];
@@ -623,7 +624,7 @@ template <View VIEW>
 hipError_t launch_few(const QCacheView& c, const ChunkAttendArgs& a, const ChunkPlan& plan, uint32_t* counters, hipStream_t st) {
   const int tiles = plan.tile_rows / 16;
   const auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)plan.workgroups), dim3(few_waves(tiles) * kWave), few_waves(tiles) * kUnitBytes, st, c.tokens, a, counters);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)plan.workgroups), dim3(few_waves(tiles) * kWave), few_waves(tiles) * kUnitBytes, st, c.tokens, a, counters, divider(c.tokens.page_size));
     return hipGetLastError();
   };
   const bool e4m3 = c.format == ROCKETKV_Q_E4M3;

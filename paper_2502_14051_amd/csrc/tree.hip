@@ -56,8 +56,7 @@ hipError_t launch_tree_mask(int batch, const ChunkView& ch, const int32_t* paren
 
 // Kept tokens together, a workgroup per (sequence, KV head).  A kept token never moves back, and what it goes over is no
 // kept token that has not been read yet: tokens are taken in order, kMoved at a time, all read before the first is written.
-// Then the summaries of the pages that changed, a thread per channel down their keys, a half of the workgroup the maxima,
-// the other the minima.
+// Then the summaries of the pages that changed, a thread per channel down their keys, the halves of the workgroup page about.
 struct KeepArgs {
   ChunkView ch;
   const uint8_t* keep;
@@ -67,6 +66,7 @@ struct KeepArgs {
 };
 
 constexpr int kMoved = 16;  // tokens moved at a time
+constexpr int kRead = 8;    // keys of a page on their way at a time
 
 template <int FMT>
 __global__ __launch_bounds__(kTreeT) void keep_kernel(CacheView c, KeepArgs a) {
@@ -155,27 +155,35 @@ __global__ __launch_bounds__(kTreeT) void keep_kernel(CacheView c, KeepArgs a) {
   const int end = old + m;
   if (a.kmax) {
     const int ch = tid % kHeadDim;
-    const bool low = tid >= kHeadDim;
-    bf16_t* out = (low ? a.kmin : a.kmax) + (((int64_t)b * c.n_kv_heads + g) * kHeadDim + ch) * c.pages_cap;
-    for (int p = old / ps; p * ps < end; ++p) {
+    const int64_t out = (((int64_t)b * c.n_kv_heads + g) * kHeadDim + ch) * c.pages_cap;
+    for (int p = old / ps + tid / kHeadDim; p * ps < end; p += kTreeT / kHeadDim) {
       const int64_t at = place(p * ps);
       if (at < 0) continue;
       const int live = min(ps, end - p * ps);
-      bf16_t best = 0;
-      for (int t = 0; t < live; ++t) {
-        bf16_t x;
-        if constexpr (CODES) {
-          const Codes8 k = load_codes<FMT>(c.k_pool, a.k_scales, at + t, ch / 8);
-          const uint4 v = restore8<FMT>(k.codes, k.scale);
-          const uint32_t w = ch % 8 < 4 ? (ch % 8 < 2 ? v.x : v.y) : (ch % 8 < 6 ? v.z : v.w);
-          x = (bf16_t)(w >> (16 * (ch % 2)));
-        } else {
-          x = c.k_pool[at + t * kHeadDim + ch];
+      bf16_t mx = 0, mn = 0;
+      for (int t0 = 0; t0 < live; t0 += kRead) {  // (the last key again in the place of those behind it)
+        bf16_t x[kRead];
+#pragma unroll
+        for (int u = 0; u < kRead; ++u) {
+          const int64_t t = min(t0 + u, live - 1);
+          if constexpr (CODES) {
+            const Codes8 k = load_codes<FMT>(c.k_pool, a.k_scales, at + t, ch / 8);
+            const uint4 v = restore8<FMT>(k.codes, k.scale);
+            const uint32_t w = ch % 8 < 4 ? (ch % 8 < 2 ? v.x : v.y) : (ch % 8 < 6 ? v.z : v.w);
+            x[u] = (bf16_t)(w >> (16 * (ch % 2)));
+          } else {
+            x[u] = c.k_pool[at + t * kHeadDim + ch];
+          }
         }
-        const float f = bf16_to_f32(x), o = bf16_to_f32(best);
-        if (t == 0 || (low ? f < o : f > o)) best = x;
+#pragma unroll
+        for (int u = 0; u < kRead; ++u) {
+          const float f = bf16_to_f32(x[u]);
+          if (t0 + u == 0 || f > bf16_to_f32(mx)) mx = x[u];
+          if (t0 + u == 0 || f < bf16_to_f32(mn)) mn = x[u];
+        }
       }
-      out[p] = best;
+      a.kmax[out + p] = mx;
+      a.kmin[out + p] = mn;
     }
   }
   // The last of the sequence's workgroups to have read its length stores the new one.

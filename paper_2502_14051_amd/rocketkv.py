@@ -710,26 +710,28 @@ class QCache:
 
     def struct(self) -> QCacheStruct:
         k, v, ks, vs, table = self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.block_table
-        width = q_row_bytes(self.format)
-        shape, strides = ks.shape, ks.stride()
-        page, head = strides[0] // 4, strides[1] // 4  # in tokens
-        rows, at = shape[:3] + (width,), (page * width, head * width, width, 1)
-        if (shape[1:] != (self.n_kv_heads, self.page_size, 4) or strides[2:] != (4, 1) or k.shape != rows or v.shape != rows or
-                vs.shape != shape or k.stride() != at or v.stride() != at or vs.stride() != strides or
-                k.element_size() + v.element_size() + ks.element_size() + vs.element_size() != 4):
-            self._refuse(width)
+        n, head = k.size(0), self.page_size
+        page = head * self.n_kv_heads  # in tokens
+        codes = n * page * (128 if self.format == Q_E4M3 else 64)
+        if not (k.is_contiguous() and v.is_contiguous() and ks.is_contiguous() and vs.is_contiguous() and
+                k.nbytes == codes and v.nbytes == codes and ks.nbytes == n * page * 4 and vs.nbytes == n * page * 4):
+            page, head = self._strides()  # (most caches are whole tensors of the right size, which is quicker to see)
         return QCacheStruct(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_size, self.pages_cap,
-                            shape[0], page, head, self.seq_lens.data_ptr(), None if table is None else table.data_ptr(),
+                            n, page, head, self.seq_lens.data_ptr(), None if table is None else table.data_ptr(),
                             k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), self.format)
 
-    def _refuse(self, width):
-        """Says which of the tensors is none a cache can have."""
+    def _strides(self):
+        """Of pages and heads, in tokens; says which of the tensors is none a cache can have."""
+        width = q_row_bytes(self.format)
         shape = (self.k_codes.shape[0], self.n_kv_heads, self.page_size)
+        page, head = (x // 4 for x in self.k_scales.stride()[:2])
         for name, t, w in (("k_codes", self.k_codes, width), ("v_codes", self.v_codes, width), ("k_scales", self.k_scales, 4),
                            ("v_scales", self.v_scales, 4)):
             if t.element_size() != 1 or t.shape != shape + (w,):
                 raise RocketKVError(INVALID_ARG, f"{name}: need bytes {shape + (w,)}, got {t.dtype} {tuple(t.shape)}")
-        raise RocketKVError(INVALID_ARG, "strides of codes and scales must be the same in tokens, rows contiguous")
+            if t.stride() != (page * w, head * w, w, 1):
+                raise RocketKVError(INVALID_ARG, f"{name}: strides must be those of k_scales in tokens, rows contiguous")
+        return page, head
 
 
 def q_row_bytes(format: int) -> int:

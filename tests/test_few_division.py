@@ -63,6 +63,11 @@ int main() {
     for (int k = 0; k < 32; ++k)
       if (pieces != (t == 1 ? 8 : t == 2 ? 16 : 32) || (t > 2 && few_begin(t * 129, k * 32 / t, pieces) % 129 && k * 32 / t < 32 && k < t)) { ++bad; printf("%d tiles: %d pieces\n", t, pieces); break; }
   }
+  for (int d = 1; d <= 64; ++d)
+    for (int i = 0; i < 200000; ++i) {
+      const uint32_t n = i < 3000 ? i : i < 6000 ? 0x7fffffffu - (i - 3000) : i < 100000 ? rnd(0x80000000u) : (uint32_t)d * rnd(0x7fffffffu / d) - (i & 1);
+      if (n < 0x80000000u && divide(n, divider(d)) != n / d) { ++bad; printf("%u / %d\n", n, d); break; }
+    }
   printf("%d cut, %d whole beside others\n", cut, crossing);
   return bad != 0 || cut < 5000 || crossing < 5000;
 }
