@@ -477,9 +477,9 @@ int32_t rocketkv_weight_evict(const rocketkv_cache_t* src, const float* weights,
  * A block's power of two is the smallest with which none of its values exceeds the largest code (2^-100 at least, and at
  * most what keeps values in the range of bf16: 2^119 for E4M3, 2^125 for E2M1, beyond which codes are the largest); a value
  * becomes the nearest code, half way the even one.  A block that holds a value that is not finite becomes NaN as a whole,
- * scale 255; other scales lie in 27 .. 246 (E4M3) or 27 .. 252 (E2M1).  Every value a code stands for is a bf16 value, so a quantised cache is exactly
- * the bf16 cache of those values in half or a quarter of the bytes, and what an operator computes on it is what its
- * counterpart computes on that cache.
+ * scale 255; other scales lie in 27 .. 246 (E4M3) or 27 .. 252 (E2M1).  Every value a code stands for is a bf16 value, so a
+ * quantised cache is exactly the bf16 cache of those values in half or a quarter of the bytes, and what an operator computes
+ * on it is what its counterpart computes on that cache.
  *
  * Both keys and values lie by token.  In each of the four pools token t of a physical page pp and KV head g is entry
  *        pp * stride_page + g * stride_head + t
@@ -571,7 +571,8 @@ int32_t rocketkv_q_chunk_attend(const rocketkv_qcache_t* cache, const rocketkv_c
 
 /*
  * rocketkv_attend over a quantised cache: one token per sequence over the listed pages of each KV head (NULL: every page).
- * A page may be listed more than once; its tokens then count as often.
+ * A page may be listed more than once; its tokens then count as often.  Entries outside 0 .. pages_cap - 1 are ignored, and
+ * tokens at or beyond seq_lens[b].  ROCKETKV_UNSUPPORTED beyond 2^30 tokens a list and 2^36 in all.
  * workspace: rocketkv_q_workspace_bytes(ROCKETKV_OP_ATTEND, cache, pages_row_len).
  */
 int32_t rocketkv_q_attend(const rocketkv_qcache_t* cache, const void* q, const int32_t* pages, int32_t pages_row_len,

@@ -1,19 +1,33 @@
 // Attention over quantised caches: of a chunk of new tokens, and of single tokens over a list of pages.
 //
 // Keys and values are widened to bf16 on their way into LDS, which is exact (a code of at most four significant bits times
-// a power of two), so what follows is the attention over bf16 caches that hold the same values.
+// a power of two), so what follows is the attention over bf16 caches that hold the same values.  The matrix cores also take
+// codes with their powers of two as they are, at twice to four times the rate; but they add such products with about 13 bits
+// (sums of 128 products were up to 2e-4 of their magnitudes off, bf16 ones 1e-7), queries and weights would have to become
+// codes too, and what most calls wait for is memory.
+//
+// Two forms.  Few rows: wavefronts with keys of their own (the attention of few rows, beside).  Many: tiles of 128 or 256 rows
+// that share every key through LDS, as over bf16 caches, but with codes requested to registers two steps ahead and widened on
+// their way to LDS, which costs vector operations beside the exponentials' (2048 tokens behind 32768, 4 heads to a KV head: 1092
+// us from 4 bits, 1040 to 1118 from bf16).
 #include "chunk_attend_core.h"
 
 namespace rkv {
 
-// Rows of a sequence on average up to which its keys are walked by wavefronts of their own.
+// Rows of a sequence on average up to which its keys are walked by wavefronts of their own.  us that way, in tiles of 128 and of
+// 256 rows, 8 KV heads of 4 query heads: 9 tokens of each of 16 sequences of 4096 in 8 bits 46, 62, 76; 16 of each of up to 32768
+// 150, 200, 200.  It holds 64 rows at most: twice that would leave a SIMD one wavefront.
 constexpr int kFewRows = 64;
+// Rows on average up to which tiles have 128 rows.  us in tiles of 128 and of 256: 32 tokens of each of 16 sequences of up to
+// 32768 in 8 bits 188, 275; 100 behind 8000 40.9, 38.7; 387 behind 131072 1178, 951; 2048 behind 32768 in 4 bits 1226, 1092; 2048
+// alone 74.9, 81.3.
+constexpr int kSmallTile = 128;
 
 ChunkPlan plan_q_attend(const QCacheView& c, int n_tokens) {
   ChunkPlan p;
   const int64_t rows = (int64_t)n_tokens * c.tokens.group / c.tokens.batch;
   p.far = p.stream = false;
-  p.tile_rows = rows <= 128 ? 128 : 256;
+  p.tile_rows = rows <= kSmallTile ? 128 : 256;
   plan_chunk_tiles(c.tokens, n_tokens, p);
   const int tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   if (rows <= kFewRows && few_units_bound(c.tokens, n_tokens, tiles) < 1ll << 31) plan_few(c.tokens, n_tokens, tiles, p);

@@ -220,6 +220,34 @@ def test_unseen_tokens_may_be_anything(fmt, ps, token_major, bad):
             m.check(out, lse)
 
 
+@pytest.mark.parametrize("fmt", qr.FORMATS)
+@pytest.mark.parametrize("hq,hkv", [(4, 2), (16, 1)])
+@pytest.mark.parametrize("kind", ["causal", "tree", "random", "none"])
+@pytest.mark.parametrize("lens,news", [([300, 90], [1, 1]), ([300, 90], [3, 2]), ([300, 90], [9, 6]), ([300, 90], [40, 20])])
+def test_unseen_codes_may_be_anything(fmt, hq, hkv, kind, lens, news):
+    """The same of quantised blocks that stand for NaN, of tiles of a single token as well."""
+    c = ref.Case(34, lens, news, hq, hkv, 16, True)
+    q = qr.take_over(c, fmt, 4)
+    seen = [torch.tril(torch.ones((n, n), dtype=torch.bool)) for n in news] if kind == "causal" else masked(8, lens, news, kind)
+    m = qr.MaskedCase(c, seen)
+    mask = None if kind == "causal" else m.mask
+    clean, clean_lse = attend(c, q, mask)
+    node, g = news[0] // 2, hkv - 1
+    t = lens[0] - news[0] + node
+    hit = torch.zeros((c.rows, hq), dtype=torch.bool, device="cuda")
+    hit[c.rows_of(0), hq // hkv * g:] = seen[0][:, node, None].cuda()
+    for scales in (q.v_scales, q.k_scales):
+        scales[int(q.block_table[0, t // 4]), g, t % 4, 2] = 255
+        out, lse = attend(c, q, mask)
+        if scales is q.v_scales:
+            assert torch.isnan(out[hit][:, 64:96]).all() and torch.equal(lse, clean_lse)
+            assert torch.equal(out[~hit], clean[~hit])
+        else:
+            assert torch.isnan(out[hit]).all() and torch.isnan(lse[hit]).all()
+            out[hit], lse[hit] = clean[hit], clean_lse[hit]
+            m.check(out, lse)
+
+
 @pytest.mark.parametrize("news", [[1], [5, 0, 33], [64, 65, 31, 200], [700], [5000, 3]])
 @pytest.mark.parametrize("late", [0.1, 0.7, 3.0])
 def test_tree_mask(news, late):
