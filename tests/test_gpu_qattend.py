@@ -482,6 +482,33 @@ def test_two_graphs_one_workspace_and_another_stream(fmt):
         ref.check_attention(c, out, lse)
 
 
+@pytest.mark.parametrize("fmt", qr.FORMATS)
+def test_more_heads_than_workgroups_fill(fmt):
+    """300 KV heads: no tile is cut."""
+    for news in ([1, 1, 1], [2, 1, 9]):
+        c = ref.Case(63, [1500, 40, 700], news, 300, 300, 16, True)
+        ref.check_attention(c, *attend(c, qr.take_over(c, fmt)))
+
+
+@pytest.mark.parametrize("fmt", qr.FORMATS)
+def test_calls_at_once(fmt):
+    """Calls on two streams, each with a workspace of its own, whose parts are joined by workgroups of the same call."""
+    cases = [ref.Case(64, [9000, 6000], [3, 1], 4, 2, 16, True), ref.Case(65, [20000], [1], 4, 2, 16, True)]
+    qs = [qr.take_over(c, fmt) for c in cases]
+    want = [attend(c, q) for c, q in zip(cases, qs)]
+    spaces = [rk.q_alloc_workspace(rk.OP_CHUNK_ATTEND, q, c.rows) for c, q in zip(cases, qs)]
+    outs = [[(torch.zeros_like(o), torch.zeros_like(l)) for _ in range(20)] for o, l in want]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for c, q, ws, out, st in zip(cases, qs, spaces, outs, streams):
+            rk.q_chunk_attend(q, c.chunk, c.q, out[i][0], out[i][1], ws, stream=st)
+    torch.cuda.synchronize()
+    for (o, l), out in zip(want, outs):
+        for got, got_lse in out:
+            assert torch.equal(got, o) and torch.equal(got_lse, l)
+
+
 def far_cache(c, fmt, ps=64):
     """The Case's tokens in a quantised cache whose rows lie beyond 4 GiB of codes, pages and heads at strides of their own."""
     per = (max(c.lens) + 40) // ps + 2
