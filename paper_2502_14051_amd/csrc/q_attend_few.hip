@@ -59,9 +59,10 @@ __device__ __forceinline__ f4 ld_agent4(float* base, uint32_t at) {
 #endif
 }
 
-// The row of all tiles' units of a KV head, and the piece a workgroup takes.
+// How the tiles of a KV head are divided, and the piece a workgroup takes.
 struct FewRow {
   int units, pieces, from, to;
+  int size;  // of parts that no two tiles share, from .. to then being counted in parts; or 0
 };
 // The part of a tile that a piece holds, units u0 .. u1 - 1 of it.
 struct FewPart {
@@ -76,59 +77,97 @@ __device__ __forceinline__ int few_tiles(const ChunkAttendArgs& a, const ChunkSe
 }
 __device__ __forceinline__ int few_units(const ChunkSeq& s) { return max(1, chunk_ceil(s.len, 32)); }  // (a tile without keys has one of none)
 
+// Lists are all of one length, so the host knows how they are divided: units of one, parts of one (0: pieces of the row).
+struct FewLists {
+  int units, pieces, parts;
+  Divider by_parts;
+};
+FewLists few_lists(int batch, int tokens, int slots) {
+  FewLists l = {max(1, chunk_ceil(tokens, 32)), 0, 0, divider(1)};
+  const int units = batch * l.units;
+  for (int i = 0; i < few_tries(units, slots) && l.parts == 0; ++i) {
+    const int parts = few_parts(l.units, few_size(units, slots, i));
+    if ((int64_t)batch * parts <= slots) l.parts = parts;
+  }
+  l.pieces = l.parts ? batch * l.parts : few_pieces(units, batch, slots);
+  l.by_parts = divider(l.parts ? l.parts : 1);
+  return l;
+}
+__device__ __forceinline__ FewRow list_row(FewLists l, int batch, int at) {
+  if (at >= l.pieces) return {0, 0, 0, 0, 0};
+  const int units = batch * l.units;
+  if (l.parts) return {units, l.pieces, at, at + 1, 0};
+  return {units, l.pieces, few_begin(units, at, l.pieces), few_begin(units, at + 1, l.pieces), 0};
+}
+// Where place `from` of the row lies in its tile: `place` of its `parts` parts, or (0) of its units.
+__device__ __forceinline__ void place_in(FewPart& p, FewRow r, int at, int from, int place, int units, int parts) {
+  int u0 = place, u1, end, first = at - place, n = parts;
+  if (parts == 1) {
+    u1 = units, end = from + 1;
+  } else if (parts) {
+    u0 = few_begin(units, place, parts), u1 = few_begin(units, place + 1, parts), end = from + 1;
+  } else {
+    const int begin = from - place;
+    end = min(r.to, begin + units), u1 = end - begin;
+    first = few_piece_of(r.units, begin, r.pieces);
+    n = few_piece_of(r.units, begin + units - 1, r.pieces) - first + 1;
+  }
+  p.u0 = u0, p.u1 = u1, p.end = end;
+  p.part = at - first, p.parts = n, p.first = first;
+}
+__device__ __forceinline__ FewPart list_part(FewLists l, FewRow r, int tokens, int at, int from) {
+  FewPart p;
+  const int parts = l.parts, units = l.units;
+  p.b = p.row = parts ? (int)divide((uint32_t)from, l.by_parts) : from / units;
+  p.n = 1, p.len = tokens, p.tile = 0;
+  place_in(p, r, at, from, from - p.b * (parts ? parts : units), units, parts);
+  return p;
+}
+
 // Both by one wavefront, a sequence a lane; `own`: of the first 64, looked up once.
 template <View VIEW>
 __device__ __forceinline__ FewRow few_row(const CacheView& c, const ChunkAttendArgs& a, const ChunkSeq& own, int at) {
-  int tiles = 0, units = 0;
-  if (VIEW == kListed) {
-    tiles = c.batch;
-    units = c.batch * max(1, chunk_ceil(a.row_len * c.page_size, 32));
-  } else {
-    const auto total = [](int x) { return __builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)x), kWave - 1); };
+  const auto each = [&](const auto& count) {  // the sum over all tiles of what count(units) says
     const int lane = threadIdx.x % kWave;
+    int sum = 0;
     for (int b0 = 0; b0 < c.batch; b0 += kWave) {
-      int t = 0, u = 0;
+      int x = 0;
       if (b0 + lane < c.batch) {
         const ChunkSeq s = b0 == 0 ? own : chunk_seq<VIEW>(c, a, b0 + lane);
-        t = few_tiles<VIEW>(a, s);
-        u = few_units(s);
+        x = few_tiles<VIEW>(a, s) * count(few_units(s));
       }
-      tiles += total(t);
-      units += total(t * u);
+      sum += __builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)x), kWave - 1);
     }
+    return sum;
+  };
+  const int units = each([](int u) { return u; });
+  const int tries = few_tries(units, a.slots);
+#pragma unroll 1
+  for (int i = 0; i < tries; ++i) {
+    const int size = few_size(units, a.slots, i), parts = each([&](int u) { return few_parts(u, size); });
+    if (parts <= a.slots) return {units, parts, at, min(at + 1, parts), size};
   }
-  const int pieces = few_pieces(units, tiles, a.slots);
-  if (at >= pieces) return {units, pieces, 0, 0};
-  return {units, pieces, few_begin(units, at, pieces), few_begin(units, at + 1, pieces)};
+  const int pieces = few_pieces(units, each([](int) { return 1; }), a.slots);
+  if (at >= pieces) return {units, pieces, 0, 0, 0};
+  return {units, pieces, few_begin(units, at, pieces), few_begin(units, at + 1, pieces), 0};
 }
 template <View VIEW>
 __device__ __forceinline__ FewPart few_part(const CacheView& c, const ChunkAttendArgs& a, const ChunkSeq& own, const FewRow& r, int at, int from) {
   FewPart p;
   ChunkSeq s;
-  int idx, u;
-  if (VIEW == kListed) {
-    s = {0, 1, a.row_len * c.page_size};
-    u = few_units(s);
-    p.b = s.row = from / u;
-    idx = from - p.b * u;
-  } else {
-    locate_tile(c.batch, from, [&](int i) {
-      const ChunkSeq s = i < kWave ? own : chunk_seq<VIEW>(c, a, i);
-      return few_tiles<VIEW>(a, s) * few_units(s);
-    }, p.b, idx);
-    if (p.b < kWave) s = {__builtin_amdgcn_readlane(own.row, p.b), __builtin_amdgcn_readlane(own.n, p.b), __builtin_amdgcn_readlane(own.len, p.b)};
-    else s = chunk_seq<VIEW>(c, a, p.b);
-    u = few_units(s);
-  }
+  int idx;
+  const auto share = [&](int u) { return r.size ? few_parts(u, r.size) : u; };  // of a tile in the row
+  locate_tile(c.batch, from, [&](int i) {
+    const ChunkSeq s = i < kWave ? own : chunk_seq<VIEW>(c, a, i);
+    return few_tiles<VIEW>(a, s) * share(few_units(s));
+  }, p.b, idx);
+  if (p.b < kWave) s = {__builtin_amdgcn_readlane(own.row, p.b), __builtin_amdgcn_readlane(own.n, p.b), __builtin_amdgcn_readlane(own.len, p.b)};
+  else s = chunk_seq<VIEW>(c, a, p.b);
+  const int u = few_units(s);
   p.row = s.row, p.n = s.n, p.len = s.len;
-  p.tile = idx / u;
-  p.u0 = idx - p.tile * u;
-  const int begin = from - p.u0, end = begin + u;
-  p.end = min(r.to, end);
-  p.u1 = p.end - begin;
-  p.first = few_piece_of(r.units, begin, r.pieces);
-  p.part = at - p.first;
-  p.parts = few_piece_of(r.units, end - 1, r.pieces) - p.first + 1;
+  const int of = share(u);
+  p.tile = idx / of;
+  place_in(p, r, at, from, idx - p.tile * of, u, r.size ? of : 0);
   return p;
 }
 
@@ -136,7 +175,7 @@ __device__ __forceinline__ FewPart few_part(const CacheView& c, const ChunkAtten
 
 template <Source SRC, View VIEW, int NB>
 __global__ __launch_bounds__(few_waves(NB) * kWave) __attribute__((amdgpu_waves_per_eu(few_per_simd(NB))))
-void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters, Divider by_page) {
+void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters, Divider by_page, FewLists all_lists) {
   constexpr int kRows = 16 * NB, kWaves = few_waves(NB);
   constexpr int kRowBytes = SRC == kE4M3 ? kHeadDim : kHeadDim / 2;
   constexpr int kKeyLoads = SRC == kE4M3 ? 2 : 1;  // of 16 bytes, a lane's 32 codes of a key
@@ -155,10 +194,10 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters, Divid
   // (lists are all of one length, and take no looking up)
   constexpr bool lists = VIEW == kListed;
   constexpr bool chunk = VIEW == kCausal || VIEW == kMasked;  // whose rows may see less than all keys of a tile
-  FewRow whole = {0, 0, 0, 0};
+  FewRow whole = {0, 0, 0, 0, 0};
   if (lists) {
-    const FewRow r = few_row<VIEW>(c, a, {0, 0, 0}, at);
-    whole = {same(r.units), same(r.pieces), same(r.from), same(r.to)};
+    const FewRow r = list_row(all_lists, c.batch, at);
+    whole = {same(r.units), same(r.pieces), same(r.from), same(r.to), same(r.size)};
   } else if (wave == 0) {
     const int lane = threadIdx.x;
     const ChunkSeq own = chunk_seq_of_lane<VIEW>(c, a);
@@ -172,7 +211,7 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters, Divid
   }
   if (!lists) {
     __syncthreads();
-    whole = {0, 0, same(s_row.from), same(s_row.to)};
+    whole = {0, 0, same(s_row.from), same(s_row.to), 0};
   }
   const int to = whole.to;
 #pragma unroll 1
@@ -180,7 +219,7 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters, Divid
     // (a lane's places are derived anew at each use: held over the loops they would take the registers that are left)
     const int tid = (int)use_late(threadIdx.x), lane = tid % kWave, i16 = lane % 16, kg = lane / 16;
     if (lists) asm volatile("" : "+s"(whole.units));  // (nor the reciprocals that divide by it)
-    const FewPart found_part = lists ? few_part<VIEW>(c, a, {0, 0, 0}, whole, at, from) : s_part;
+    const FewPart found_part = lists ? list_part(all_lists, whole, a.row_len * ps, at, from) : s_part;
     const FewPart pl = {same(found_part.b), same(found_part.row), same(found_part.n), same(found_part.len), same(found_part.tile),
                         same(found_part.u0), same(found_part.u1), same(found_part.end), same(found_part.part),
                         same(found_part.parts), same(found_part.first)};
@@ -627,7 +666,7 @@ void plan_few(const CacheView& c, int n_tokens, int tiles, ChunkPlan& p) {
   p.tile_tokens = p.tile_rows / c.group;
   int64_t most_tiles = (int64_t)n_tokens / p.tile_tokens + c.batch;
   if (most_tiles > n_tokens) most_tiles = n_tokens;
-  p.slots = few_pieces((int)few_units_bound(c, n_tokens, tiles), (int)most_tiles, c.n_kv_heads < kFewMost ? kFewMost / c.n_kv_heads : 1);
+  p.slots = few_most((int)few_units_bound(c, n_tokens, tiles), (int)most_tiles, c.n_kv_heads < kFewMost ? kFewMost / c.n_kv_heads : 1);
   p.most = 2 * p.slots * c.n_kv_heads;
   p.cuts = p.slots > 1;
   p.workgroups = (int64_t)p.slots * c.n_kv_heads;
@@ -637,8 +676,10 @@ namespace {
 template <View VIEW>
 hipError_t launch_few(const QCacheView& c, const ChunkAttendArgs& a, const ChunkPlan& plan, uint32_t* counters, hipStream_t st) {
   const int tiles = plan.tile_rows / 16;
+  const FewLists lists = VIEW == kListed ? few_lists(c.tokens.batch, a.row_len * c.tokens.page_size, a.slots) : FewLists{0, a.slots, 0, {0, 0}};
   const auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)plan.workgroups), dim3(few_waves(tiles) * kWave), few_waves(tiles) * kUnitBytes, st, c.tokens, a, counters, divider(c.tokens.page_size));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(lists.pieces * c.tokens.n_kv_heads)), dim3(few_waves(tiles) * kWave), few_waves(tiles) * kUnitBytes, st, c.tokens, a,
+                       counters, divider(c.tokens.page_size), lists);
     return hipGetLastError();
   };
   const bool e4m3 = c.format == ROCKETKV_Q_E4M3;

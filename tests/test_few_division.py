@@ -57,6 +57,33 @@ int main() {
     for (int k = 0; k < pieces; ++k)
       if (goes_on[k] > 1 || went_on[k] > 1) { ++bad; printf("trial %d: piece %d has no place\n", trial, k); }
   }
+  // parts of tiles that nothing else shares
+  int whole = 0, own = 0, fits[2] = {0, 0};
+  for (int trial = 0; trial < 40000 && bad < 10; ++trial) {
+    const int slots = 1 + rnd(256), n = 1 + rnd(trial % 2 ? 300 : 12), longest = 1 + rnd(trial % 4 == 0 ? 60000 : trial % 3 == 0 ? 60 : 600);
+    int sum = 0;
+    for (int t = 0; t < n; ++t) sum += units[t] = 1 + (trial % 5 == 0 ? longest - 1 : rnd(longest));
+    for (int i = 0; i < kFewTries; ++i) {
+      const int size = few_size(sum, slots, i);
+      if (size < kFewRound || (int64_t)size * slots < sum) { ++bad; printf("trial %d: size %d\n", trial, size); }
+      int64_t parts = 0;
+      for (int t = 0; t < n; ++t) parts += few_parts(units[t], size);
+      if (parts > slots) continue;
+      ++fits[i];
+      if (parts > few_most(sum, n, 256)) { ++bad; printf("trial %d: %d parts\n", trial, (int)parts); }
+      for (int t = 0; t < n; ++t) {
+        const int k = few_parts(units[t], size);
+        ++(k == 1 ? whole : own);
+        for (int j = 0; j < k; ++j) {
+          const int len = few_begin(units[t], j + 1, k) - few_begin(units[t], j, k);
+          if (len < 1 || (k > 1 && len > size)) { ++bad; printf("trial %d: part of %d\n", trial, len); }
+        }
+        if (few_begin(units[t], 0, k) != 0 || few_begin(units[t], k, k) != units[t]) { ++bad; printf("trial %d: ends of parts\n", trial); }
+      }
+      break;
+    }
+  }
+  if (whole < 5000 || own < 5000 || fits[0] < 1000 || fits[1] < 1000) { ++bad; printf("%d whole, %d cut, sizes %d %d\n", whole, own, fits[0], fits[1]); }
   // equal tiles: as many pieces to each as fit, none across two
   for (int t = 1; t <= 32; t *= 2) {
     const int pieces = few_pieces(t * 129, t, 32);
