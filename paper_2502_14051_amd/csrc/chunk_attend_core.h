@@ -544,25 +544,29 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
   // Where there are such values among partly seen keys, the unit's keys with any are added one by one, for the rows that
   // see them, and leave the operand.
   const auto keep_future_out = [&](int key0, u32x4 (&vf)[2][4], u32x4 (&pf)[2]) {
-    uint32_t odd = 0;  // bit 8 y + e: key 16 y + 8 h + e has one among this lane's channels
+    // an exponent of ones carries into its value's sign
+    const auto signs = [](uint32_t pair) { return (pair & 0x7f807f80u) + 0x00800080u; };
+    uint32_t odd = 0;
 #pragma unroll
     for (int y = 0; y < 2; ++y)
 #pragma unroll
       for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          odd |= (vf[y][cb][i] & 0x7f80u) == 0x7f80u ? 1u << (8 * y + 2 * i) : 0u;
-          odd |= (vf[y][cb][i] & 0x7f800000u) == 0x7f800000u ? 2u << (8 * y + 2 * i) : 0u;
-        }
-    if (!__any(odd != 0u)) return;
+        for (int i = 0; i < 4; ++i) odd |= signs(vf[y][cb][i]);
+    if (!__any((odd & 0x80008000u) != 0u)) return;
     const uint32_t bits = VIEW == kMasked ? seen_bits(key0) : 0u;
 #pragma unroll
     for (int y = 0; y < 2; ++y)
 #pragma unroll 1
       for (int k = 0; k < 16; ++k) {  // key 16 y + k, element k % 8 of the lanes of half k / 8
-        if (!__any(h == k / 8 && (odd >> (8 * y + k % 8) & 1u))) continue;
         const uint32_t mine = h == k / 8 ? k & 1 ? 0xffff0000u : 0xffffu : 0u;
         const u32x4 sel = {k % 8 / 2 == 0 ? mine : 0u, k % 8 / 2 == 1 ? mine : 0u, k % 8 / 2 == 2 ? mine : 0u, k % 8 / 2 == 3 ? mine : 0u};
+        odd = 0;
+#pragma unroll
+        for (int cb = 0; cb < 4; ++cb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) odd |= signs(vf[y][cb][i] & sel[i]);
+        if (!__any((odd & 0x80008000u) != 0u)) continue;
         const bool seen = VIEW == kMasked ? (bits >> (16 * y + k) & 1u) != 0u : key0 + 16 * y + k <= last;
 #pragma unroll
         for (int cb = 0; cb < 4; ++cb) {
