@@ -23,18 +23,6 @@ __device__ __forceinline__ int converted(const CacheView& src, const CacheView& 
   return n < 0 || n > cap ? 0 : n;
 }
 
-template <int FMT>
-__device__ __forceinline__ Codes8 quantise_bf16(const uint4& v) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  float x[8];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = bf16lo_to_f32(w[i]);
-    x[2 * i + 1] = bf16hi_to_f32(w[i]);
-  }
-  return quantise8<FMT>(x);
-}
-
 // By channel, lanes 2c and 2c + 1 of a half of the workgroup hold channel c's tokens 0..7 and 8..15 of a tile.
 struct TileLane {
   int channel, first;
@@ -93,8 +81,8 @@ __global__ __launch_bounds__(kConvT) void quantise_kernel(ConvertArgs a) {
       v[u] = make_uint4(in[0], in[1], in[2], in[3]);
     }
     if (to[u] >= 0) {
-      store_codes<FMT>(dst.k_pool, a.k_scales, to[u], lane16, quantise_bf16<FMT>(k[u]));
-      store_codes<FMT>(dst.v_pool, a.v_scales, to[u], lane16, quantise_bf16<FMT>(v[u]));
+      store_codes<FMT>(dst.k_pool, a.k_scales, to[u], lane16, quantise8<FMT>(k[u]));
+      store_codes<FMT>(dst.v_pool, a.v_scales, to[u], lane16, quantise8<FMT>(v[u]));
     }
   }
 }

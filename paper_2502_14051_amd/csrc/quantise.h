@@ -62,6 +62,47 @@ __device__ __forceinline__ Codes8 quantise8(const float (&x)[8]) {
   return r;
 }
 
+// The same from bf16, whose conversions divide by the scale and round once as well.  What exceeds the largest code, which only
+// the highest power of two for E4M3 leaves (above 1.75 x 2^127), they would make NaN.
+template <int FMT>
+__device__ __forceinline__ Codes8 quantise8(const uint4& v) {
+  [[maybe_unused]] constexpr bool kEight = FMT == ROCKETKV_Q_E4M3;
+  Codes8 r = {make_uint2(0u, 0u), 0u};
+#ifdef __HIP_DEVICE_COMPILE__
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  const auto size = [](uint32_t pair) { return __builtin_bit_cast(u16x2, pair & 0x7fff7fffu); };
+  const u16x2 most = __builtin_elementwise_max(__builtin_elementwise_max(size(w[0]), size(w[1])), __builtin_elementwise_max(size(w[2]), size(w[3])));
+  const uint32_t m = block_max_u32(max((uint32_t)most.x, (uint32_t)most.y)) << 16;
+  const int scale = min(max((int)((m + (kEight ? 0x1fffffu : 0x3fffffu)) >> 23) - (kEight ? 8 : 2), 27), kEight ? 246 : 252);
+  const float by = __uint_as_float((uint32_t)scale << 23);
+  if (kEight && __any(m > 0x7f600000u)) {
+    const u16x2 limit = {0x7f60, 0x7f60};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (w[i] & 0x80008000u) | __builtin_bit_cast(uint32_t, __builtin_elementwise_min(size(w[i]), limit));
+  }
+  const auto pair = [&](int i) { return __builtin_bit_cast(bf16x2, w[i]); };
+  if constexpr (kEight) {
+    s16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(s16x2{0, 0}, pair(0), by, false);
+    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, pair(1), by, true);
+    s16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(s16x2{0, 0}, pair(2), by, false);
+    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, pair(3), by, true);
+    r.codes = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+  } else {
+    uint32_t x = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, pair(0), by, 0);
+    x = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(x, pair(1), by, 1);
+    x = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(x, pair(2), by, 2);
+    x = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(x, pair(3), by, 3);
+    r.codes.x = x;
+  }
+  r.scale = (uint32_t)scale;
+  if (m >= 0x7f800000u) r = {make_uint2(0u, 0u), 255u};
+#endif
+  return r;
+}
+
 // What eight codes stand for, in bf16, exactly.  (The conversion takes the scale's exponent alone; the highest gives NaN.)
 template <int FMT>
 __device__ __forceinline__ uint4 restore8(uint2 codes, uint32_t scale) {

@@ -20,6 +20,7 @@ constexpr int kRowLanes = kHeadDim / 8;     // lanes that hold a head row, eight
 constexpr int kRowsPerPass = kRopeT / kRowLanes;
 constexpr int kBlockTokens = 32;            // tokens whose sines are in LDS at a time
 constexpr int kRowsInFlight = 4;            // rows a thread has requested at once
+constexpr int kFewBlocks = 1024;            // workgroups below which blocks of pages become smaller
 
 typedef uint32_t rope_u32x4 __attribute__((ext_vector_type(4)));
 
@@ -262,8 +263,8 @@ void append_chunk_kernel(CacheView c, AppendChunkArgs a) {
           const int i = i0 + u * kRowsPerPass, t = tl + i;
           if constexpr (FMT != kBf16) {
             if (t < th) {
-              const Codes8 k = quantise8<FMT>(turns ? turn8(a.rope, kp[u], s_cs + i * half, c0).x : unpack8(kp[u].own).x);
-              const Codes8 v = quantise8<FMT>(unpack8(vp[u]).x);
+              const Codes8 k = turns ? quantise8<FMT>(turn8(a.rope, kp[u], s_cs + i * half, c0).x) : quantise8<FMT>(kp[u].own);
+              const Codes8 v = quantise8<FMT>(vp[u]);
               if (a.kmax) *reinterpret_cast<uint4*>(s_k + i * (kHeadDim / 2) + c0 / 2) = restore8<FMT>(k.codes, k.scale);
               const int64_t pp = phys_page(c, b, t / ps);
               if (pp >= 0) {
@@ -356,7 +357,7 @@ void append_chunk_kernel(CacheView c, AppendChunkArgs a) {
     if (a.kmax && lo < hi) {
       __syncthreads();
       const int first = lo / ps - p0, last = (hi - 1) / ps - p0;  // pages that took in a token
-      const int groups = a.pages / 8;
+      const int groups = (a.pages + 7) / 8;
       for (int i = tid; i < ng * 2 * kHeadDim * groups; i += kRopeT) {
         const int pg = i % groups * 8, row = i / groups;  // row: (head, extreme, channel)
         const int chn = row % kHeadDim, gi = row / (2 * kHeadDim);
@@ -416,7 +417,7 @@ __global__ __launch_bounds__(kRopeT) void put_chunk_kernel(CacheView c, AppendCh
 #pragma unroll
       for (int u = 0; u < kPutRows; ++u) {
         if (t0 + u >= hi) break;
-        const Codes8 kc = quantise8<FMT>(unpack8(k[u]).x), vc = quantise8<FMT>(unpack8(v[u]).x);
+        const Codes8 kc = quantise8<FMT>(k[u]), vc = quantise8<FMT>(v[u]);
         if (pp >= 0) {
           store_codes<FMT>(c.k_pool, a.k_scales, tok + t0 + u, lane16, kc);
           store_codes<FMT>(c.v_pool, a.v_scales, tok + t0 + u, lane16, vc);
@@ -515,6 +516,10 @@ hipError_t launch_append_any(const CacheView& c, uint8_t* k_scales, uint8_t* v_s
     return (int)(x < ch.n_tokens ? x : ch.n_tokens);
   };
   while (pages > 8 && (int64_t)blocks(pages) * c.n_kv_heads < 1024) pages -= 8;
+  // A block's tokens come kBlockTokens at a time, one lot after the other: fewer pages, where that would leave the chip idle.
+  // (Into 8 bits, 8 KV heads, us so and with 8 pages: 159 tokens of each of 2 sequences 15 and 31, 64 of each of 16 18 and 23,
+  // 2048 of one 43 and 50; up to 2000 of each of 4, pages of 64, 40 and 142.)
+  while (pages > 1 && pages * c.page_size > kBlockTokens && (int64_t)blocks(pages) * c.n_kv_heads < kFewBlocks) pages /= 2;
   a.pages = pages;
   a.kv_wgs = blocks(pages);
   a.heads_per_wg = c.n_kv_heads < 4 ? c.n_kv_heads : 4;
