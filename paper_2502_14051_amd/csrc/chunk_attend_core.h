@@ -381,7 +381,8 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
   };
 
   // Codes come to registers, are widened there and go to LDS as bf16 rows would lie: eight lanes a row, 16 channels each.
-  // They are requested a whole step before that, the values of a step together with the keys of the next.
+  // They are requested a whole step before that, the values of a step together with the keys of the next.  A key is widened
+  // once for the rows of a workgroup, about 2 x 20 vector operations a lane and step beside the 2 x 60 of its exponentials.
   constexpr int kPieces = 8 / WAVES;  // rows of a step a lane brings a piece of
   constexpr int kRowBytes = SRC == kE4M3 ? kHeadDim : kHeadDim / 2;
   typedef typename Codes16<SRC>::Raw Raw;

@@ -8,9 +8,10 @@
 // 19.4, 16.8, 14.7, 14.1.)
 // (A token of each of 8 sequences of up to 5211, one KV head, 17.3 us so and 25.1 in equal pieces of all; of 16 of up to 3000, 8
 // KV heads, 23.7 and 29.7: a workgroup whose piece holds the end of one tile and the beginning of another does both in turn.)
-// Where that would leave workgroups idle, or they have many rounds to take, the units of all tiles of a KV head stand in a row, tile behind tile, and
-// every workgroup takes an equal piece of it, wherever that begins and ends: lengths may differ as they like.  A tile that lies
-// in several pieces has that many parts, whose results are joined; of a piece only the first and the last tile can be such.
+// Where that would leave workgroups idle, or they have many rounds to take, the units of all tiles of a KV head stand in a row,
+// tile behind tile, and every workgroup takes an equal piece of it, wherever that begins and ends: lengths may differ as they
+// like.  A tile that lies in several pieces has that many parts, whose results are joined; of a piece only the first and the
+// last tile can be such.
 #pragma once
 #include <stdint.h>
 

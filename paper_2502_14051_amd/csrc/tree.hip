@@ -11,7 +11,8 @@ constexpr int kTreeNodes = 4096;  // of a sequence whose parents are kept in LDS
 }  // namespace
 
 // A thread per row walks up its tree.  Parents stand before their children, so the words of its mask are met from the last
-// to the first and each is written once.  A walk is a chain of reads, of LDS but for parents beyond kTreeNodes.
+// to the first and each is written once.  A walk is a chain of reads, of LDS but for parents beyond kTreeNodes, and as long as
+// the tree is deep: latency is all there is to it (16 trees of 32 rows 4.8 us, one of 200 5.4, a launch of next to nothing 2.5).
 __global__ __launch_bounds__(kTreeT) void tree_mask_kernel(ChunkView ch, const int32_t* __restrict__ parents,
                                                            const int32_t* __restrict__ base, uint32_t* __restrict__ bits,
                                                            int words, int32_t* __restrict__ positions) {
@@ -57,6 +58,9 @@ hipError_t launch_tree_mask(int batch, const ChunkView& ch, const int32_t* paren
 // Kept tokens together, a workgroup per (sequence, KV head).  A kept token never moves back, and what it goes over is no
 // kept token that has not been read yet: tokens are taken in order, kMoved at a time, all read before the first is written.
 // Then the summaries of the pages that changed, a thread per channel down their keys, the halves of the workgroup page about.
+// Few bytes and a chain of round trips: the length, the flags, the pages, the rows, the keys of the pages that changed (5 of 32
+// tokens of 16 sequences, 8 heads, bf16 6.6 us; 9 of 200 in pages of 4 in 8 bits 6.7; 7.2 and 7.9 with a page's keys requested
+// one after the other).
 struct KeepArgs {
   ChunkView ch;
   const uint8_t* keep;
