@@ -16,7 +16,7 @@ namespace rkv {
 
 // Rows of a sequence on average up to which its keys are walked by wavefronts of their own.  us that way, in tiles of 128 and of
 // 256 rows, 8 KV heads of 4 query heads: 9 tokens of each of 16 sequences of 4096 in 8 bits 46, 62, 76; 16 of each of up to 32768
-// 150, 200, 200.  It holds 64 rows at most: twice that would leave a SIMD one wavefront.
+// 150, 200, 200.  64 rows at most: the sums of twice as many do not fit a wavefront's registers.
 constexpr int kFewRows = 64;
 // Rows on average up to which tiles have 128 rows.  us in tiles of 128 and of 256: 32 tokens of each of 16 sequences of up to
 // 32768 in 8 bits 188, 275; 100 behind 8000 40.9, 38.7; 387 behind 131072 1178, 951; 2048 behind 32768 in 4 bits 1226, 1092; 2048
