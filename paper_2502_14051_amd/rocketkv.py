@@ -710,11 +710,11 @@ class QCache:
 
     def struct(self) -> QCacheStruct:
         k, v, ks, vs, table = self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.block_table
-        n, head = k.size(0), self.page_size
+        n, head, width = k.size(0), self.page_size, 128 if self.format == Q_E4M3 else 64
         page = head * self.n_kv_heads  # in tokens
-        codes = n * page * (128 if self.format == Q_E4M3 else 64)
-        if not (k.is_contiguous() and v.is_contiguous() and ks.is_contiguous() and vs.is_contiguous() and
-                k.nbytes == codes and v.nbytes == codes and ks.nbytes == n * page * 4 and vs.nbytes == n * page * 4):
+        codes, scales = n * page * width, n * page * 4
+        if not (k.shape == (n, self.n_kv_heads, head, width) and k.is_contiguous() and v.is_contiguous() and ks.is_contiguous() and
+                vs.is_contiguous() and k.nbytes == codes and v.nbytes == codes and ks.nbytes == scales and vs.nbytes == scales):
             page, head = self._strides()  # (most caches are whole tensors of the right size, which is quicker to see)
         return QCacheStruct(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_size, self.pages_cap,
                             n, page, head, self.seq_lens.data_ptr(), None if table is None else table.data_ptr(),

@@ -238,3 +238,12 @@ def test_binding_looks_at_tensors():
         rk.q_attend(q, t[:2], torch.zeros((2, 3, 4), dtype=torch.int32), t[:2].clone(), None, ws)
     with pytest.raises(rk.RocketKVError, match="parents"):
         rk.tree_mask(ch, torch.zeros(4, dtype=torch.int32), rk.alloc_mask(5, 5, "cpu"))
+
+
+def test_caches_of_another_layout_are_refused():
+    """As many bytes in another order of dimensions, or of another type, are no cache."""
+    for bad in (torch.zeros((16, 4, 2, 128), dtype=torch.uint8), torch.zeros((16, 2, 4, 64), dtype=torch.bfloat16)):
+        q = rk.alloc_qcache(2, 8, 2, 4, 8, "cpu")
+        q.k_codes = bad
+        with pytest.raises(rk.RocketKVError, match="k_codes"):
+            q.struct()
