@@ -19,15 +19,18 @@ namespace rkv {
 // 150, 200, 200.  64 rows at most: the sums of twice as many do not fit a wavefront's registers.
 constexpr int kFewRows = 64;
 // Rows on average up to which tiles have 128 rows.  us in tiles of 128 and of 256: 32 tokens of each of 16 sequences of up to
-// 32768 in 8 bits 188, 275; 100 behind 8000 40.9, 38.7; 387 behind 131072 1178, 951; 2048 behind 32768 in 4 bits 1226, 1092; 2048
-// alone 74.9, 81.3.
+// 32768 in 8 bits 188, 275; 100 behind 8000 43, 40; 387 behind 131072 1178, 951; 2048 behind 32768 in 4 bits 1226, 1092.
 constexpr int kSmallTile = 128;
+// Tokens a sequence has room for up to which they do too, as it is workgroups that such short rows of keys lack: prompts of up
+// to 472 of one head 20.3, 24.2; 200 behind 1000 in 4 bits 24.2, 28.9; 64 of each of 16 behind 1000 46, 52; 2000 alone in 8 bits
+// 76, 78; but 4000 alone in 4 bits 182, 167, 8000 in 8 bits 607, 565, 500 behind 4000 68, 65.
+constexpr int kShortCache = 2048;
 
 ChunkPlan plan_q_attend(const QCacheView& c, int n_tokens) {
   ChunkPlan p;
   const int64_t rows = (int64_t)n_tokens * c.tokens.group / c.tokens.batch;
   p.far = p.stream = false;
-  p.tile_rows = rows <= kSmallTile ? 128 : 256;
+  p.tile_rows = rows <= kSmallTile || (int64_t)c.tokens.pages_cap * c.tokens.page_size <= kShortCache ? 128 : 256;
   plan_chunk_tiles(c.tokens, n_tokens, p);
   const int tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   if (rows <= kFewRows && few_units_bound(c.tokens, n_tokens, tiles) < 1ll << 31) plan_few(c.tokens, n_tokens, tiles, p);

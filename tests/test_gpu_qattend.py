@@ -70,6 +70,21 @@ def test_tiles_beside_the_chip(fmt, news, lens):
 
 
 @pytest.mark.parametrize("fmt", qr.FORMATS)
+@pytest.mark.parametrize("news,lens", [([640, 700], [700, 1500]), ([300, 3, 400], [900, 1400, 400]), ([40], [40])])
+@pytest.mark.parametrize("kind", ["causal", "tree", "random"])
+def test_tiles_where_there_is_room_for_more(fmt, news, lens, kind):
+    """The same over caches that could hold more than 2048 tokens of a sequence, which take the larger tiles; and by masks."""
+    c = ref.Case(23, lens, news, 16, 2, 16, True)
+    q = qr.take_over(c, fmt, 16, spare=130)
+    assert q.pages_cap * 16 > 2048
+    if kind == "causal":
+        ref.check_attention(c, *attend(c, q))
+    else:
+        m = qr.MaskedCase(c, masked(24, lens, news, kind))
+        m.check(*attend(c, q, m.mask))
+
+
+@pytest.mark.parametrize("fmt", qr.FORMATS)
 @pytest.mark.parametrize("hq,hkv", [(8, 2), (3, 1), (16, 1), (40, 8)])
 @pytest.mark.parametrize("lens,news", [
     ([60] * 5 + [300], [1] * 5 + [60]),          # single tokens, and a sequence of many tiles among them
@@ -223,11 +238,12 @@ def test_unseen_tokens_may_be_anything(fmt, ps, token_major, bad):
 @pytest.mark.parametrize("fmt", qr.FORMATS)
 @pytest.mark.parametrize("hq,hkv", [(4, 2), (16, 1)])
 @pytest.mark.parametrize("kind", ["causal", "tree", "random", "none"])
-@pytest.mark.parametrize("lens,news", [([300, 90], [1, 1]), ([300, 90], [3, 2]), ([300, 90], [9, 6]), ([300, 90], [40, 20])])
-def test_unseen_codes_may_be_anything(fmt, hq, hkv, kind, lens, news):
+@pytest.mark.parametrize("lens,news,room", [([300, 90], [1, 1], 0), ([300, 90], [3, 2], 0), ([300, 90], [9, 6], 0), ([300, 90], [40, 20], 0),
+                                            ([300, 200], [150, 90], 0), ([300, 200], [150, 90], 500)])
+def test_unseen_codes_may_be_anything(fmt, hq, hkv, kind, lens, news, room):
     """The same of quantised blocks that stand for NaN, of tiles of a single token as well."""
     c = ref.Case(34, lens, news, hq, hkv, 16, True)
-    q = qr.take_over(c, fmt, 4)
+    q = qr.take_over(c, fmt, 4, spare=room)
     seen = [torch.tril(torch.ones((n, n), dtype=torch.bool)) for n in news] if kind == "causal" else masked(8, lens, news, kind)
     m = qr.MaskedCase(c, seen)
     mask = None if kind == "causal" else m.mask
