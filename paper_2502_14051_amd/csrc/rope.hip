@@ -20,6 +20,7 @@ constexpr int kRowLanes = kHeadDim / 8;     // lanes that hold a head row, eight
 constexpr int kRowsPerPass = kRopeT / kRowLanes;
 constexpr int kBlockTokens = 32;            // tokens whose sines are in LDS at a time
 constexpr int kRowsInFlight = 4;            // rows a thread has requested at once
+constexpr int kQueryRows = 128;             // of a block of queries of few tokens
 constexpr int kFewBlocks = 1024;            // workgroups below which blocks of pages become smaller
 
 typedef uint32_t rope_u32x4 __attribute__((ext_vector_type(4)));
@@ -519,8 +520,8 @@ hipError_t launch_append_any(const CacheView& c, uint8_t* k_scales, uint8_t* v_s
   };
   while (pages > 8 && (int64_t)blocks(pages) * c.n_kv_heads < 1024) pages -= 8;
   // A block's tokens come kBlockTokens at a time, one lot after the other: fewer pages, where that would leave the chip idle.
-  // (Into 8 bits, 8 KV heads, us so and with 8 pages: 159 tokens of each of 2 sequences 15 and 31, 64 of each of 16 18 and 23,
-  // 2048 of one 43 and 50; up to 2000 of each of 4, pages of 64, 40 and 142.)
+  // (Into 8 bits, 8 KV heads, us so and with 8 pages: 159 tokens of each of 2 sequences 15 and 31, 64 of each of 16 18 and 23;
+  // up to 2000 of each of 4 in pages of 64, before the queries' blocks grew as below, 40 and 142.)
   while (pages > 1 && pages * c.page_size > kBlockTokens && (int64_t)blocks(pages) * c.n_kv_heads < kFewBlocks) pages /= 2;
   a.pages = pages;
   a.kv_wgs = blocks(pages);
@@ -528,7 +529,13 @@ hipError_t launch_append_any(const CacheView& c, uint8_t* k_scales, uint8_t* v_s
   while (a.heads_per_wg > 1 && (int64_t)a.kv_wgs * ((c.n_kv_heads + a.heads_per_wg - 1) / a.heads_per_wg) < 1024) a.heads_per_wg /= 2;
   while (a.heads_per_wg > 1 && a.heads_per_wg * 2 * kHeadDim * pages * 2 > 32 * 1024) a.heads_per_wg /= 2;
   a.head_groups = (c.n_kv_heads + a.heads_per_wg - 1) / a.heads_per_wg;
-  a.q_block = ch.n_tokens >= 32 * 2048 ? kBlockTokens : (ch.n_tokens + 2047) / 2048;
+  // Queries in 2048 blocks at most, and fewer of up to kQueryRows rows: workgroups that find their places and form sines for a
+  // token or two come in more rounds.  (2048 tokens of 32 heads into 8 bits 30 us so, 42 in 2048 blocks; 600 17, 20; 4942 of each
+  // of 2 of 8 heads 58, 64; but 4000 of 64 heads in blocks of 512 rows 35, of 128 33.)
+  const int few_tokens = kQueryRows / c.n_q_heads < 1 ? 1 : kQueryRows / c.n_q_heads;
+  a.q_block = (ch.n_tokens + 511) / 512 < few_tokens ? (ch.n_tokens + 511) / 512 : few_tokens;
+  if (a.q_block < (ch.n_tokens + 2047) / 2048) a.q_block = (ch.n_tokens + 2047) / 2048;
+  if (a.q_block > kBlockTokens) a.q_block = kBlockTokens;
   const int64_t q_blocks = q ? (int64_t)ch.n_tokens / a.q_block + c.batch : 0;
   const int q_wgs = (int)(q_blocks < ch.n_tokens ? q_blocks : (q ? ch.n_tokens : 0));
   const size_t lds = (size_t)kBlockTokens * kHeadDim / 2 * sizeof(float2) + (FMT == kBf16 ? 2 : 1) * (size_t)kBlockTokens * kHeadDim * sizeof(bf16_t) +
