@@ -60,6 +60,14 @@ RKV_HD inline int few_piece_of(int units, int x, int pieces) {
   return k + (few_begin(units, k + 1, pieces) <= x);
 }
 
+// Units of all tiles at most: `rows` tokens of `batch` sequences in tiles of `tile_tokens`, of caches with room for `room` tokens.
+// What a launch has places for, and 32 bits count.  It holds where the rows of the sequences add up to `rows` at most; rows that
+// two sequences share (starts that do not ascend) can come to any number of units, so a launch that finds more does nothing.
+RKV_HD inline int64_t few_bound(int rows, int batch, int tile_tokens, int64_t room) {
+  const int64_t tiles = (int64_t)rows / tile_tokens + batch;
+  return (tiles < rows ? tiles : rows) * ((room + 31) / 32);
+}
+
 // Division of numbers below 2^31 by the same one again and again: n / d = (hi(n m) + n) >> l with l = ceil(log2 d) and
 // m = floor(2^32 (2^l - d) / d) + 1 (Granlund and Montgomery 1994).
 struct Divider {

@@ -129,20 +129,24 @@ __device__ __forceinline__ FewPart list_part(FewLists l, FewRow r, int tokens, i
 // Both by one wavefront, a sequence a lane; `own`: of the first 64, looked up once.
 template <View VIEW>
 __device__ __forceinline__ FewRow few_row(const CacheView& c, const ChunkAttendArgs& a, const ChunkSeq& own, int at) {
-  const auto each = [&](const auto& count) {  // the sum over all tiles of what count(units) says
+  const auto each = [&](const auto& count, int64_t* rows = nullptr) {  // the sum over all tiles of what count(units) says
     const int lane = threadIdx.x % kWave;
-    int sum = 0;
+    uint32_t sum = 0;
     for (int b0 = 0; b0 < c.batch; b0 += kWave) {
-      int x = 0;
+      uint32_t x = 0, n = 0;
       if (b0 + lane < c.batch) {
         const ChunkSeq s = b0 == 0 ? own : chunk_seq<VIEW>(c, a, b0 + lane);
-        x = few_tiles<VIEW>(a, s) * count(few_units(s));
+        n = (uint32_t)s.n;
+        x = (uint32_t)few_tiles<VIEW>(a, s) * (uint32_t)count(few_units(s));
       }
-      sum += __builtin_amdgcn_readlane((int)wave_incl_scan((uint32_t)x), kWave - 1);
+      sum += (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan(x), kWave - 1);
+      if (rows) *rows += __builtin_amdgcn_readlane((int)wave_incl_scan(n), kWave - 1);
     }
-    return sum;
+    return (int)sum;
   };
-  const int units = each([](int u) { return u; });
+  int64_t rows = 0;
+  const int units = VIEW == kWhole ? each([](int u) { return u; }) : each([](int u) { return u; }, &rows);
+  if (rows > a.ch.n_tokens) return {0, 0, 0, 0, 0};  // (more than was planned for, see few_bound)
   const int tries = few_tries(units, a.slots);
 #pragma unroll 1
   for (int i = 0; i < tries; ++i) {
@@ -159,10 +163,11 @@ __device__ __forceinline__ FewPart few_part(const CacheView& c, const ChunkAtten
   ChunkSeq s;
   int idx;
   const auto share = [&](int u) { return r.size ? few_parts(u, r.size) : u; };  // of a tile in the row
-  locate_tile(c.batch, from, [&](int i) {
-    const ChunkSeq s = i < kWave ? own : chunk_seq<VIEW>(c, a, i);
-    return few_tiles<VIEW>(a, s) * share(few_units(s));
-  }, p.b, idx);
+  if (!locate_tile(c.batch, from, [&](int i) {
+        const ChunkSeq s = i < kWave ? own : chunk_seq<VIEW>(c, a, i);
+        return few_tiles<VIEW>(a, s) * share(few_units(s));
+      }, p.b, idx))
+    return FewPart{};  // (no rows; lengths that something else changes meanwhile)
   if (p.b < kWave) s = {__builtin_amdgcn_readlane(own.row, p.b), __builtin_amdgcn_readlane(own.n, p.b), __builtin_amdgcn_readlane(own.len, p.b)};
   else s = chunk_seq<VIEW>(c, a, p.b);
   const int u = few_units(s);
@@ -225,6 +230,7 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters, Divid
     const FewPart pl = {same(found_part.b), same(found_part.row), same(found_part.n), same(found_part.len), same(found_part.tile),
                         same(found_part.u0), same(found_part.u1), same(found_part.end), same(found_part.part),
                         same(found_part.parts), same(found_part.first)};
+    if (!lists && pl.n == 0) return;
     const ChunkSeq s = {pl.row, pl.n, pl.len};
     from = pl.end;
     const int t0 = pl.tile * a.tile_tokens, nt = min(a.tile_tokens, s.n - t0);
@@ -657,9 +663,7 @@ void few_attend_kernel(CacheView c, ChunkAttendArgs a, uint32_t* counters, Divid
 }
 
 int64_t few_units_bound(const CacheView& c, int n_tokens, int tiles) {
-  const int tile_tokens = 16 * tiles / c.group;
-  const int64_t most_tiles = (int64_t)n_tokens / tile_tokens + c.batch;
-  return (most_tiles < n_tokens ? most_tiles : n_tokens) * (((int64_t)c.pages_cap * c.page_size + kUnit - 1) / kUnit);
+  return few_bound(n_tokens, c.batch, 16 * tiles / c.group, (int64_t)c.pages_cap * c.page_size);
 }
 
 void plan_few(const CacheView& c, int n_tokens, int tiles, ChunkPlan& p) {

@@ -1,0 +1,68 @@
+"""Chunks whose `starts` do not ascend: results are not defined, but nothing out of range is read or written."""
+import pytest
+import torch
+
+import chunk_ref as ref
+import quant_ref as qr
+from paper_2502_14051_amd import rocketkv as rk
+
+pytestmark = pytest.mark.gpu
+
+GUARD = 4096  # rows around what a call is given
+
+
+def guarded(rows, heads, width, dtype):
+    whole = torch.full((rows + 2 * GUARD, heads) + width, 7.0, dtype=dtype, device="cuda")
+    return whole, whole[GUARD:GUARD + rows]
+
+
+def untouched(whole):
+    return bool((whole[:GUARD] == 7).all()) and bool((whole[-GUARD:] == 7).all())
+
+
+def call(q, starts, n, mask):
+    """Rows and results in the middle of larger tensors; a fresh workspace, whose counters are not defined afterwards."""
+    all_q, rows = guarded(n, q.n_q_heads, (128,), torch.bfloat16)
+    all_out, out = guarded(n, q.n_q_heads, (128,), torch.bfloat16)
+    all_lse, lse = guarded(n, q.n_q_heads, (), torch.float32)
+    rows.normal_()
+    ws = rk.q_alloc_workspace(rk.OP_CHUNK_ATTEND, q, n)
+    m = rk.Mask(torch.full((n, 1), -1, dtype=torch.int32, device="cuda")) if mask else None
+    rk.q_chunk_attend(q, rk.Chunk(torch.tensor(starts, dtype=torch.int32, device="cuda"), n), rows, out, lse, ws, mask=m)
+    torch.cuda.synchronize()
+    assert untouched(all_q) and untouched(all_out) and untouched(all_lse)
+
+
+@pytest.mark.parametrize("fmt", qr.FORMATS)
+@pytest.mark.parametrize("mask", [False, True])
+@pytest.mark.parametrize("starts", [[0, 6, 1, 7], [7, 5, 2, 0], [0, 7, 0, 7], [-5, 100, -3, 50], [3, 3, 2, 7], [1 << 30, -(1 << 30), 1 << 30, 0]])
+def test_few_rows(fmt, mask, starts):
+    c = ref.Case(41, [300, 40, 2000], [2, 1, 4], 8, 2, 16, True)
+    call(qr.take_over(c, fmt), starts, c.rows, mask)
+
+
+@pytest.mark.parametrize("fmt", qr.FORMATS)
+@pytest.mark.parametrize("mask", [False, True])
+def test_few_rows_of_more_units_than_32_bits_count(fmt, mask):
+    """2048 sequences of 131072 tokens, which share their pages; every other one has all of 131072 rows: 2^33 units of keys."""
+    batch, ps, cap = 2048, 64, 2048
+    table = torch.arange(cap, dtype=torch.int32, device="cuda").repeat(batch, 1)
+    q = rk.alloc_qcache(batch, 1, 1, ps, cap, "cuda", fmt, table, cap)
+    for x in (q.k_codes, q.v_codes):
+        x.zero_()
+    for x in (q.k_scales, q.v_scales):
+        x.fill_(127)
+    q.seq_lens.fill_(ps * cap)
+    n = 64 * batch
+    call(q, [n * (b % 2) for b in range(batch + 1)], n, mask)
+
+
+@pytest.mark.parametrize("fmt", qr.FORMATS)
+def test_gaps_between_sequences_are_no_overlap(fmt):
+    """Rows in front, behind, and as many as there are; sequences of none."""
+    c = ref.Case(42, [300, 40, 2000, 64], [2, 0, 4, 1], 8, 2, 16, True, pad=(3, 2))
+    q = qr.take_over(c, fmt)
+    out = torch.full((c.rows, c.hq, ref.D), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((c.rows, c.hq), 7.0, device="cuda")
+    rk.q_chunk_attend(q, c.chunk, c.q, out, lse, rk.q_alloc_workspace(rk.OP_CHUNK_ATTEND, q, c.rows))
+    ref.check_attention(c, out, lse)
