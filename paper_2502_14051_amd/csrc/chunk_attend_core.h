@@ -214,7 +214,7 @@ __device__ __forceinline__ int chunk_size_for(const CacheView& c, const ChunkAtt
     }
   };
   each([&](int t, int steps) {
-    load.tiles += total(t) * c.n_kv_heads;
+    load.tiles = chunk_add_tiles(load.tiles, total(t), c.n_kv_heads, a.most);
     // (a coarser count keeps the sums in range where sequences are long: 2^15 steps are 2^21 tokens)
     load.work += (float)total(min(t, a.most) * min(steps, 1 << 15)) * (float)c.n_kv_heads;
     load.longest = max(load.longest, (int)wave_max_u32((uint32_t)steps));

@@ -30,7 +30,7 @@ RKV_HD constexpr int chunk_ceil(int a, int b) { return a / b + (a % b != 0); }
 RKV_HD constexpr int chunk_parts(int steps, int size) { return steps <= size ? 1 : chunk_ceil(steps, size); }
 
 struct ChunkLoad {
-  int tiles;    // row tiles of all sequences and KV heads
+  int tiles;    // row tiles of all sequences and KV heads, see chunk_add_tiles
   float work;   // steps of all of them
   int longest;  // steps of the longest
 };
@@ -40,6 +40,13 @@ struct ChunkLoad {
 // average, 10 % at most).  From half as many tiles as slots on, one round has no room to cut, and 129 to 255 tiles would
 // leave up to half of the chip idle: three, so that 192 tiles come as quarters.
 RKV_HD constexpr int chunk_rounds(int64_t tiles, int slots) { return 2 * tiles > slots ? kChunkRounds : 1; }
+
+// `tiles` and `more` of each of `heads`, counted up to `most`, from which on nothing is cut.  (Sequences whose rows overlap, of
+// starts that do not ascend, can come to more than 32 bits count; a count that had wrapped would cut keys into parts that the
+// merge looks for behind the end of the workspace.)
+RKV_HD constexpr int chunk_add_tiles(int tiles, int more, int heads, int most) {
+  return tiles + (int64_t)more * heads < most ? tiles + more * heads : most;
+}
 
 // Steps per part.  `slots`: workgroups the chip holds at a time, `most`: a multiple of it that the result does not exceed
 // unless the tiles do; `count(size)`: workgroups at that size.

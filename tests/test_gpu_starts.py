@@ -22,13 +22,20 @@ def untouched(whole):
 
 def call(q, starts, n, mask):
     """Rows and results in the middle of larger tensors; a fresh workspace, whose counters are not defined afterwards."""
+    codes = isinstance(q, rk.QCache)
     all_q, rows = guarded(n, q.n_q_heads, (128,), torch.bfloat16)
     all_out, out = guarded(n, q.n_q_heads, (128,), torch.bfloat16)
     all_lse, lse = guarded(n, q.n_q_heads, (), torch.float32)
     rows.normal_()
-    ws = rk.q_alloc_workspace(rk.OP_CHUNK_ATTEND, q, n)
+    ws = (rk.q_alloc_workspace if codes else rk.alloc_workspace)(rk.OP_CHUNK_ATTEND, q, n)
     m = rk.Mask(torch.full((n, 1), -1, dtype=torch.int32, device="cuda")) if mask else None
-    rk.q_chunk_attend(q, rk.Chunk(torch.tensor(starts, dtype=torch.int32, device="cuda"), n), rows, out, lse, ws, mask=m)
+    chunk = rk.Chunk(torch.tensor(starts, dtype=torch.int32, device="cuda"), n)
+    if codes:
+        rk.q_chunk_attend(q, chunk, rows, out, lse, ws, mask=m)
+    elif mask:
+        rk.masked_attend(q, chunk, m, rows, out, lse, ws)
+    else:
+        rk.chunk_attend(q, chunk, rows, out, lse, ws)
     torch.cuda.synchronize()
     assert untouched(all_q) and untouched(all_out) and untouched(all_lse)
 
@@ -55,6 +62,14 @@ def test_few_rows_of_more_units_than_32_bits_count(fmt, mask):
     q.seq_lens.fill_(ps * cap)
     n = 64 * batch
     call(q, [n * (b % 2) for b in range(batch + 1)], n, mask)
+
+
+@pytest.mark.parametrize("fmt", [None] + qr.FORMATS)
+@pytest.mark.parametrize("mask", [False, True])
+@pytest.mark.parametrize("starts", [[0, 1000, 0, 1000], [1000, 500, 400, 0], [0, 900, 100, 1000], [-5, 2000, -3, 50]])
+def test_tiles(fmt, mask, starts):
+    c = ref.Case(43, [1300, 40, 9000], [500, 0, 500], 8, 2, 16, True)
+    call(c.cache if fmt is None else qr.take_over(c, fmt), starts, c.rows, mask)
 
 
 @pytest.mark.parametrize("fmt", qr.FORMATS)
