@@ -530,7 +530,9 @@ int32_t rocketkv_q_append_chunk(const rocketkv_qcache_t* cache, const rocketkv_c
 /*
  * Which tokens of a chunk each of them sees, in place of those up to its own: row i of a sequence's rows sees its row j if
  * bit j % 32 of word j / 32 of its words is set (rows from 32 * words on are seen by none), itself only if its own bit is.
- * What the cache held before the chunk is seen by all.  Trees of drafted tokens, and any other pattern.
+ * What the cache held before the chunk is seen by all.  Trees of drafted tokens, and any other pattern.  Of a sequence with
+ * more rows than tokens the last rows are the tokens; those in front of them are in no cache and seen by none, but see, as all
+ * do, the tokens that their own bits name.
  * bits: device uint32 [n_tokens][words].  The struct lives in host memory.
  */
 typedef struct rocketkv_mask {

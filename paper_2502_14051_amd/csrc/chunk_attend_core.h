@@ -278,10 +278,10 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
   const int steps = chunk_ceil(max(0, VIEW == kMasked ? s.len : min(s.len, pos0 + nt)), kStep), per = chunk_ceil(steps, pl.parts);
   const int it0 = min(pl.part * per, steps), it1 = min(it0 + per, steps);
 
-  // this lane's row: its query in registers, and the last key it sees
+  // this lane's row: its query in registers, and the last key it sees (kMasked: -1 if there is no such row, and unused else)
   const int r = wave * 32 + col;
   const bool working = wave * 32 < rows;
-  const int last = r < rows ? pos0 + r / G : -1;
+  const int last = r < rows ? VIEW == kMasked ? 0 : pos0 + r / G : -1;
   const auto packed_row = [&](int r) {  // (token, head) of the packed tensors
     const int t = r / G;
     return (int64_t)(s.row + t0 + t) * c.n_q_heads + (int64_t)g * G + (r - t * G);
