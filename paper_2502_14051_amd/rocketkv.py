@@ -538,12 +538,17 @@ class Rope:
 _dtypes = {}
 
 
-def _tensor(name, t, dtype, shape, rows=False):
-    """What a pointer cannot say: type, shape and layout, contiguous or, with `rows`, tokens at any stride."""
-    want = _dtypes.get(dtype)
+def _dtype(name):
+    want = _dtypes.get(name)
     if want is None:
         import torch
-        want = _dtypes[dtype] = getattr(torch, dtype)
+        want = _dtypes[name] = getattr(torch, name)
+    return want
+
+
+def _tensor(name, t, dtype, shape, rows=False):
+    """What a pointer cannot say: type, shape and layout, contiguous or, with `rows`, tokens at any stride."""
+    want = _dtypes.get(dtype) or _dtype(dtype)
     have = t.shape
     if t.dtype is not want or have != shape:
         raise RocketKVError(INVALID_ARG, f"{name}: need {dtype} {tuple(shape)}, got {t.dtype} {tuple(have)}")
@@ -709,26 +714,34 @@ class QCache:
     format: int = Q_E4M3
 
     def struct(self) -> QCacheStruct:
-        k, v, ks, vs, table = self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.block_table
-        n, head, width = k.size(0), self.page_size, 128 if self.format == Q_E4M3 else 64
+        k, v, ks, vs, lens, table = self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.seq_lens, self.block_table
+        shape, byte, i32 = k.shape, _dtypes.get("uint8") or _dtype("uint8"), _dtypes.get("int32") or _dtype("int32")
+        n, head, width = shape[0], self.page_size, 128 if self.format == Q_E4M3 else 64
         page = head * self.n_kv_heads  # in tokens
-        codes, scales = n * page * width, n * page * 4
-        if not (k.shape == (n, self.n_kv_heads, head, width) and k.is_contiguous() and v.is_contiguous() and ks.is_contiguous() and
-                vs.is_contiguous() and k.nbytes == codes and v.nbytes == codes and ks.nbytes == scales and vs.nbytes == scales):
-            page, head = self._strides()  # (most caches are whole tensors of the right size, which is quicker to see)
+        small = (n, self.n_kv_heads, head, 4)
+        if not (shape == (n, self.n_kv_heads, head, width) and v.shape == shape and ks.shape == small and vs.shape == small and
+                k.dtype is byte and v.dtype is byte and ks.dtype is byte and vs.dtype is byte and
+                k.is_contiguous() and v.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()):
+            page, head = self._strides()  # (most caches are whole tensors of the right shape, which is quicker to see)
+        if lens is not None and not (lens.dtype is i32 and lens.shape == (self.batch,) and lens.is_contiguous()):
+            _tensor("seq_lens", lens, "int32", (self.batch,))
+        if table is not None and not (table.dtype is i32 and table.shape == (self.batch, self.pages_cap) and table.is_contiguous()):
+            _tensor("block_table", table, "int32", (self.batch, self.pages_cap))
         return QCacheStruct(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_size, self.pages_cap,
-                            n, page, head, self.seq_lens.data_ptr(), None if table is None else table.data_ptr(),
+                            n, page, head, _ptr(lens), None if table is None else table.data_ptr(),
                             k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), self.format)
 
     def _strides(self):
         """Of pages and heads, in tokens; says which of the tensors is none a cache can have."""
         width = q_row_bytes(self.format)
         shape = (self.k_codes.shape[0], self.n_kv_heads, self.page_size)
-        page, head = (x // 4 for x in self.k_scales.stride()[:2])
-        for name, t, w in (("k_codes", self.k_codes, width), ("v_codes", self.v_codes, width), ("k_scales", self.k_scales, 4),
-                           ("v_scales", self.v_scales, 4)):
+        pools = (("k_codes", self.k_codes, width), ("v_codes", self.v_codes, width), ("k_scales", self.k_scales, 4),
+                 ("v_scales", self.v_scales, 4))
+        for name, t, w in pools:
             if t.element_size() != 1 or t.shape != shape + (w,):
                 raise RocketKVError(INVALID_ARG, f"{name}: need bytes {shape + (w,)}, got {t.dtype} {tuple(t.shape)}")
+        page, head = (x // 4 for x in self.k_scales.stride()[:2])
+        for name, t, w in pools:
             if t.stride() != (page * w, head * w, w, 1):
                 raise RocketKVError(INVALID_ARG, f"{name}: strides must be those of k_scales in tokens, rows contiguous")
         return page, head
