@@ -21,7 +21,7 @@ constexpr int kRowsPerPass = kRopeT / kRowLanes;
 constexpr int kBlockTokens = 32;            // tokens whose sines are in LDS at a time
 constexpr int kRowsInFlight = 4;            // rows a thread has requested at once
 constexpr int kQueryRows = 128;             // of a block of queries of few tokens
-constexpr int kFewBlocks = 1024;            // workgroups below which blocks of pages become smaller
+constexpr int kFewBlocks = 432;             // workgroups with tokens below which blocks of pages become smaller
 
 typedef uint32_t rope_u32x4 __attribute__((ext_vector_type(4)));
 
@@ -179,9 +179,9 @@ __device__ __forceinline__ NewTokens new_tokens(const CacheView& c, const ChunkV
 
 }  // namespace
 
-// New tokens into the cache, in one launch: the first workgroups take blocks of `pages` pages (aligned to `pages`, a multiple
-// of eight, so that a channel's summaries leave as whole 16-byte pieces) of some heads, the others blocks of query rows (with
-// the two kinds mixed instead, 131072 tokens take 797 us, so 706).  A block is worked through kBlockTokens tokens at a time: sines of the tokens, then head by head the key rows
+// New tokens into the cache, in one launch: the first workgroups take blocks of `pages` pages (aligned to `pages`; where that is
+// eight or more, a multiple of eight, a channel's summaries leave as whole 16-byte pieces) of some heads, the others blocks of
+// query rows (with the two kinds mixed instead, 131072 tokens take 797 us, so 706).  A block is worked through kBlockTokens tokens at a time: sines of the tokens, then head by head the key rows
 // (turned) and the value rows to the pools and to LDS, from where a thread takes a pair of channels down the tokens of a
 // page: extremes of the keys, in the order of the tokens as single appends would fold them, and the 16 values of a
 // channel-major tile's row.  Quantised caches take codes instead, by token, and LDS the values these stand for.
@@ -519,10 +519,17 @@ hipError_t launch_append_any(const CacheView& c, uint8_t* k_scales, uint8_t* v_s
     return (int)(x < ch.n_tokens ? x : ch.n_tokens);
   };
   while (pages > 8 && (int64_t)blocks(pages) * c.n_kv_heads < 1024) pages -= 8;
-  // A block's tokens come kBlockTokens at a time, one lot after the other: fewer pages, where that would leave the chip idle.
-  // (Into 8 bits, 8 KV heads, us so and with 8 pages: 159 tokens of each of 2 sequences 15 and 31, 64 of each of 16 18 and 23;
-  // up to 2000 of each of 4 in pages of 64, before the queries' blocks grew as below, 40 and 142.)
-  while (pages > 1 && pages * c.page_size > kBlockTokens && (int64_t)blocks(pages) * c.n_kv_heads < kFewBlocks) pages /= 2;
+  // A block's tokens come kBlockTokens at a time, one lot after the other: fewer pages, where that would leave the chip idle, a
+  // block more of each sequence than its tokens fill taken for half empty.  bf16, 32 heads over 8, pages of 16, with a launch that
+  // sets the lengths back, us in blocks of 8 and of 4 pages by the workgroups of 8: 48.2 and 41.6 (5000 tokens, 320), 49.2 and
+  // 48.0 (6000, 376), 44.4 and 36.6 (300 of each of 16 sequences, 424), but 49.5 and 53.7 (7000, 440), 57.5 and 61.8 (8192, 520),
+  // 62.9 and 67.9 (10000, 632).  In blocks of 8 pages and of those taken: 64 of each of 16 23 and 16.5, 159 of each of 2 25 and
+  // 14.4, 2048 in pages of 64 129 and 28; into 8 bits 4000 of 64 heads in 2 pages 56, in 4 50.
+  const auto filled = [&](int pages) {
+    const int64_t x = (int64_t)ch.n_tokens / (pages * c.page_size) + c.batch;
+    return x < ch.n_tokens ? x : ch.n_tokens;
+  };
+  while (pages > 1 && pages * c.page_size > kBlockTokens && filled(pages) * c.n_kv_heads < kFewBlocks) pages /= 2;
   a.pages = pages;
   a.kv_wgs = blocks(pages);
   a.heads_per_wg = c.n_kv_heads < 4 ? c.n_kv_heads : 4;
