@@ -50,7 +50,7 @@ enum Source { kByChannel, kByToken, kE4M3, kE2M1 };  // bf16 by the layout of th
 enum View {
   kCausal,  // the tokens up to its own
   kMasked,  // those in front of the chunk, and of the chunk those its bits say
-  kListed,  // one row per sequence: the tokens of a list of pages
+  kListed,  // one row per sequence: the tokens of a list of pages (few rows alone, as the next)
   kWhole    // one row per sequence: all of its tokens
 };
 
@@ -246,7 +246,7 @@ __device__ __forceinline__ bool chunk_place(const CacheView& c, const ChunkAtten
   return true;
 }
 
-// STREAM: keys and values past the caches.  FAR: 64 bits of offset to them.
+// STREAM: keys and values past the caches.  FAR: 64 bits of offset to them.  (Both of bf16 caches alone.)
 template <Source SRC, bool FAR, int WAVES, bool STREAM, View VIEW>
 __global__ __launch_bounds__(WAVES * kWave) __attribute__((amdgpu_waves_per_eu(2)))
 void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
@@ -415,7 +415,7 @@ void chunk_attend_kernel(CacheView c, ChunkAttendArgs a) {
       const uint32_t ln = use_late((uint32_t)lane);
       const uint32_t at = (uint32_t)__shfl((int)tok_at, (int)(piece_row(ln) + 8 * p));
       const Raw* src = reinterpret_cast<const Raw*>(reinterpret_cast<const char*>(pool) + (uint64_t)at * kRowBytes) + ln % 8;
-      to.codes[p] = STREAM ? __builtin_nontemporal_load(src) : *src;
+      to.codes[p] = *src;
       to.scales[p] = scales[at];
     }
   };
