@@ -81,3 +81,39 @@ def test_gaps_between_sequences_are_no_overlap(fmt):
     lse = torch.full((c.rows, c.hq), 7.0, device="cuda")
     rk.q_chunk_attend(q, c.chunk, c.q, out, lse, rk.q_alloc_workspace(rk.OP_CHUNK_ATTEND, q, c.rows))
     ref.check_attention(c, out, lse)
+
+
+def pool(n, *tail):
+    """Bytes of n pages, and what lies around them."""
+    whole = torch.full((n + 8,) + tail, 7, dtype=torch.uint8, device="cuda")
+    return whole, whole[4:-4]
+
+
+@pytest.mark.parametrize("fmt", qr.FORMATS)
+@pytest.mark.parametrize("turned", [False, True])
+@pytest.mark.parametrize("starts", [[0, 600, 0, 600], [600, 400, 200, 0], [0, 550, 50, 600], [-5, 1000, -3, 300]])
+def test_append_and_keep(fmt, turned, starts):
+    """Into pools with other memory in front and behind, of sequences at their last pages."""
+    n, ps, cap = 600, 4, 160
+    sides = [pool(3 * cap, 2, ps, w) for w in (rk.q_row_bytes(fmt), rk.q_row_bytes(fmt), 4, 4)]
+    q = rk.QCache(3, 8, 2, 128, ps, cap, *(inner for _, inner in sides), torch.tensor([40, 0, 400], dtype=torch.int32, device="cuda"), None, fmt)
+    all_k, k = guarded(n, 2, (128,), torch.bfloat16)
+    all_q, rows = guarded(n, 8, (128,), torch.bfloat16)
+    all_out, out = guarded(n, 8, (128,), torch.bfloat16)
+    k.normal_(), rows.normal_()
+    sums = [torch.full((3, 3, 2, 128, cap), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]  # [1] is the call's
+    chunk = rk.Chunk(torch.tensor(starts, dtype=torch.int32, device="cuda"), n)
+    rope = rk.rope_frequencies(128, 10000.0, device="cuda") if turned else None
+    kw = dict(rope=rope, q=rows, q_out=out) if turned else {}
+    rk.q_append_chunk(q, chunk, k, k, sums[0][1], sums[1][1], rk.q_alloc_workspace(rk.OP_APPEND_CHUNK, q, n), **kw)
+    keep = torch.arange(n, device="cuda") % 3 == 0
+    rk.q_keep_tokens(q, chunk, keep, sums[0][1], sums[1][1], rk.q_alloc_workspace(rk.OP_APPEND_CHUNK, q, n))
+    parents = torch.arange(n, dtype=torch.int32, device="cuda") - 1
+    bits = torch.full((n + 2 * GUARD, 19), 7, dtype=torch.int32, device="cuda")
+    where = torch.full((n + 2 * GUARD,), 7, dtype=torch.int32, device="cuda")
+    rk.tree_mask(chunk, parents, rk.Mask(bits[GUARD:GUARD + n]), q.seq_lens, where[GUARD:GUARD + n])
+    torch.cuda.synchronize()
+    assert all(untouched(x) for x in (all_k, all_q, all_out, bits, where))
+    assert all(bool((whole[:4] == 7).all()) and bool((whole[-4:] == 7).all()) for whole, _ in sides)
+    assert all(bool((s[::2] == 7).all()) for s in sums)
+    assert ((q.seq_lens >= 0) & (q.seq_lens <= cap * ps)).all()
